@@ -368,6 +368,96 @@ int svdq_w8a8_linear_forward(const svdq_layer_dev *layer, const void *X, int M, 
 int svdq_w8a8_debug_act(const svdq_layer_dev *layer, const void *workspace, int M,
                         int8_t *out_codes, uint16_t *out_sx, float *out_H, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Between a block's QKV layer and its output layer: keys and values in a paged cache of 8 bits, and attention over it.
+ *
+ * The cache.  Pages of page_tokens tokens (32, 64, ..., 1024), cut into blocks of 32; for every block and head one scale byte
+ * (value 2^(byte - 127), 0 marks a block of zeros) and 32 x head_dim E4M3 codes, keys and values apart.  A code c stands for
+ * c * 2^(byte - 127).  The buffers are the caller's device memory, 16-byte aligned (svdq_kv_cache_sizes); the codes are "native":
+ *   k_codes [pages][kv_heads][page_tokens / 32][32][head_dim]
+ *   v_codes [pages][kv_heads][page_tokens / 32][head_dim / 32][16][4][2][8]: token t and channel d of a block at
+ *           [d / 32][d % 16][2 (t / 16) + (t % 8) / 4][(d % 32) / 16][4 ((t % 16) / 8) + t % 4]
+ *   k_scales, v_scales [pages][kv_heads][page_tokens / 32]
+ * A sequence's block table names its pages in order: token i lies in page block_table[i / page_tokens].  No page belongs to two
+ * sequences that are appended to in one call, or by calls that overlap.
+ *   quantizer: byte = that of the smallest power of two s >= 2^-126 with max|x| <= 448 s over the block's tokens and channels, codes =
+ *   the E4M3 number nearest to x / s, ties to even.  A block that is filled over several calls keeps the larger of its byte and the new
+ *   tokens'; if it grows, the codes in the block are divided by the same power of two and rounded again.  A token whose key or value of a
+ *   head has an element that is not finite is left out of the maximum and held as NaN codes of the key and zeros of the value: the rows of
+ *   queries that see it are NaN, no others.
+ *
+ * The batch (svdq_kv_batch).  Sequence b has the new tokens cu_new[b] .. cu_new[b + 1] - 1 of the input (cu_new[0] = 0, cu_new[sequences]
+ * = new_tokens) as its last ones: kv_len[b] counts its tokens with them, token i of the n new ones has position kv_len[b] - n + i.
+ * The three arrays are device memory that the host does not look at; the kernels take cu_new within 0 .. new_tokens, kv_len within 0 ..
+ * table_width * page_tokens, and an entry of the block table outside 0 .. pages - 1 as no page: nothing is written there, tokens there are
+ * not seen.  New tokens in excess of kv_len have no position: they are not written and see no key.
+ *
+ * The rotation (svdq_kv_rope, NULL for none).  table: device fp32 [positions][dims], 16-byte aligned: dims / 2 cosines and dims / 2 sines
+ * of each position; dims a multiple of 16 up to head_dim.  Pairs (i, i + dims / 2), or (2 i, 2 i + 1) if interleaved:
+ * (a, b) -> (a cos - b sin, b cos + a sin) in fp32; channels from dims on stay.  A position past the table takes its last row.
+ *
+ * head_dim is 64, 128 or 256.  All inputs are bf16 with channels next to each other and any token and head stride that keeps 16-byte
+ * alignment (multiples of 8 elements), such as the columns of a fused QKV output.  Everything is enqueued on hip_stream; nothing is
+ * allocated or synchronised.  SVDQ_EINVAL: a null or misaligned pointer, a negative size, a stride off 8, window < 0, q_heads not a multiple
+ * of kv_heads.  SVDQ_EUNSUPPORTED: another head_dim or page size, more than 2^30 tokens of a sequence, 65535 heads or sequences, or 2^31 - 1
+ * work items.  SVDQ_ENOSPACE: a workspace smaller than the size query says.
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct {
+    int kv_heads, head_dim, page_tokens;
+} svdq_kv_shape;
+typedef struct {
+    size_t codes;  /* of k_codes, and of v_codes */
+    size_t scales; /* of k_scales, and of v_scales */
+} svdq_kv_sizes;
+typedef struct {
+    void *k_codes, *v_codes, *k_scales, *v_scales; /* device */
+    int pages;
+    svdq_kv_shape shape;
+} svdq_kv_cache_dev;
+typedef struct {
+    const int32_t *cu_new, *kv_len, *block_table; /* device: [sequences + 1], [sequences], [sequences][table_width] */
+    int sequences, table_width;
+    int new_tokens; /* of all sequences */
+    int max_new;    /* no sequence has more new tokens (attention: chooses the kernel; tokens past it are refused a row) */
+    int max_len;    /* no kv_len is larger (attention: how the keys are cut; larger ones are right, but slower) */
+} svdq_kv_batch;
+typedef struct {
+    const float *table; /* device */
+    int positions, dims, interleaved;
+} svdq_kv_rope;
+typedef struct {
+    const void *data; /* device bf16 [tokens][heads][head_dim] with the strides below, in elements */
+    int64_t token_stride, head_stride;
+} svdq_kv_rows;
+
+int svdq_kv_cache_sizes(const svdq_kv_shape *shape, int pages, svdq_kv_sizes *out);
+
+/* Writes the batch's new keys (rotated) and values into the cache.  One kernel; appending the same tokens again gives the same bytes. */
+int svdq_kv_append(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope,
+                   const svdq_kv_rows *k, const svdq_kv_rows *v, void *hip_stream);
+
+/*
+ * Attention of the batch's new tokens over the cache, which holds them already:
+ *   O = softmax(scale Q' K^T) V,  Q' = Q rotated;  query head h reads key head h / (q_heads / kv_heads).
+ *   causal: position p sees positions 0 .. p, with window > 0 only the last `window` of them; otherwise all kv_len.
+ * Scores, softmax statistics and sums are fp32; rotated queries and the weights exp(s - max) are rounded to f16 (11 bits, scaled
+ * so that none is lost to its range), codes times scales are exact.  A row that sees no key is zero.
+ *   out: device bf16 [new_tokens][q_heads][head_dim], 16-byte aligned
+ *   workspace: device, 256-byte aligned, >= svdq_kv_attention_workspace_bytes(); needs no initial contents.  Two calls that share one must be ordered on one stream.
+ * One kernel.
+ */
+size_t svdq_kv_attention_workspace_bytes(const svdq_kv_shape *shape, int q_heads, int sequences, int max_new, int max_len);
+int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope, const svdq_kv_rows *q,
+                      int q_heads, float scale, int causal, int window, void *out, void *workspace, size_t workspace_bytes,
+                      void *hip_stream);
+
+/*
+ * Rows of the cache as bf16 [rows][kv_heads][head_dim] (16-byte aligned; either output may be NULL): sequence b's tokens first_token[b] ..
+ * onwards are rows cu_rows[b] .. cu_rows[b + 1] - 1.  Exact where code * scale is a normal bf16.  Zeros where the table names no page.
+ */
+int svdq_kv_gather(const svdq_kv_cache_dev *cache, const int32_t *first_token, const int32_t *cu_rows, const int32_t *block_table,
+                   int sequences, int table_width, int rows, void *out_k, void *out_v, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -2,8 +2,9 @@
 
 ``paper_2411_05007_amd.svdq`` is the thin binding over the C-ABI library
 ``libsvdq.so`` (HIP kernels for gfx950 + host-side offline quantization);
+``paper_2411_05007_amd.kv`` binds its paged 8-bit cache of keys and values;
 ``paper_2411_05007_amd.inputs`` generates the seeded synthetic layers.
 Importing this package does not load the native library; the binding does, and
 it raises if the library has not been built.
 """
-__all__ = ["inputs", "svdq"]
+__all__ = ["inputs", "kv", "svdq"]

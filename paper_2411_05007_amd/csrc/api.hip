@@ -19,6 +19,11 @@ int hip_fail(hipError_t e) {
     g_last_hip_error = (int)e;
     return SVDQ_EHIP;
 }
+}  // namespace
+namespace svdq {
+int record_hip_error(hipError_t e) { return hip_fail(e); }
+}  // namespace svdq
+namespace {
 
 int check_layer(const svdq_layer_dev *L, int group = svdq::kGroup) {
     if (!L) return SVDQ_EINVAL;

@@ -200,4 +200,57 @@ struct DebugActW8Params {
 };
 hipError_t launch_debug_act_w8(const DebugActW8Params &p, hipStream_t stream);
 
+int record_hip_error(hipError_t e);      // what svdq_last_hip_error returns on this thread; returns SVDQ_EHIP (api.hip)
+
+// ---- paged 8-bit cache of keys and values (kv_common.h has the layout) ----
+struct KvCache {
+    uint8_t *k, *v;          // codes
+    uint8_t *ks, *vs;        // scale bytes [pages][heads][page / 32]
+    int pages, heads, dim, page_shift;      // dim: 64, 128 or 256; page = 1 << page_shift tokens
+};
+struct KvBatch {
+    const int32_t *cu;       // [sequences + 1]: where a sequence's new tokens (or rows) start
+    const int32_t *kv_len;   // [sequences]: tokens in the cache with the new ones.  Gather: the first token that is read
+    const int32_t *table;    // [sequences][table_width]: pages
+    int sequences, table_width, total;      // total: new tokens (rows) in all
+};
+struct KvRope {
+    const float *table;      // [positions][dims]: dims / 2 cosines, dims / 2 sines
+    int positions, dims, interleaved;       // dims = 0: no rotation
+};
+struct KvRows {              // bf16 [token][head][dim], strides in elements
+    const uint16_t *data;
+    long long token_stride, head_stride;
+};
+struct KvAppendParams {
+    KvCache cache;
+    KvBatch batch;
+    KvRope rope;
+    KvRows k, v;
+};
+hipError_t launch_kv_append(const KvAppendParams &p, hipStream_t stream);
+struct KvGatherParams {
+    KvCache cache;
+    KvBatch batch;
+    uint16_t *k, *v;         // bf16 [total][heads][dim], either may be null
+};
+hipError_t launch_kv_gather(const KvGatherParams &p, hipStream_t stream);
+struct KvAttentionParams {
+    KvCache cache;
+    KvBatch batch;
+    KvRope rope;
+    KvRows q;
+    uint16_t *out;           // bf16 [total][q_heads][dim]
+    int q_heads, group;      // group = q_heads / cache.heads
+    float scale;             // of the scores, times log2(e)
+    int causal, window;      // window = 0: none
+    int row_tiles;           // few-row kernel: tiles of 16 rows a sequence and head may need
+    int chunk_blocks, chunks;      // few-row kernel: the keys are cut into chunks of chunk_blocks blocks (the last takes the rest)
+    float *partial;          // chunks > 1: fp32 [sequence][row tile][head][chunk][16][dim], then maxima and sums [...][16][2]
+    float *partial_ml;
+    unsigned long long *arrived;      // chunks > 1: [sequence][row tile][head][chunk]
+};
+hipError_t launch_kv_attention_rows(const KvAttentionParams &p, hipStream_t stream);      // few rows (kv_rows_kernel.hip)
+hipError_t launch_kv_attention_tile(const KvAttentionParams &p, hipStream_t stream);      // many (kv_tile_kernel.hip)
+
 }  // namespace svdq

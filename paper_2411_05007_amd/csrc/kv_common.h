@@ -1,0 +1,174 @@
+// What the kernels of the paged 8-bit cache of keys and values share: the cache's layout, the work items of a ragged batch, the
+// position rotation, the conversions to and from E4M3 codes.
+//
+// A cache has pages of P tokens (32 to 1024, a power of two), cut into blocks of 32 tokens, and a scale byte for each block and head
+// (value 2^(byte - 127), 0: a block of zeros), keys and values apart.  The codes of one block and head are 32 D bytes in a row:
+//   keys    [32][D]: a row of a block is the operand row of K Q^T as it lies
+//   values  [D / 32][16][4][2][8], transposed: element (t, d) at [d / 32][d % 16][g][(d % 32) / 16][j], slot g = 2 (t / 16) + (t % 8) / 4,
+//           j = 4 ((t % 16) / 8) + t % 4.  The accumulators of S^T = K Q^T on 32 x 32 blocks hold the tokens of slots 2 s + h, s = 0, 1, in lane
+//           half h, eight in the order of j: they are the operand of O^T = V^T P^T with no exchange between lanes.
+// Why E4M3 with powers of two: gfx950 turns two codes and a power of two into two exact f16 (or bf16) numbers in one instruction; a
+// power of two can grow while its block fills without a second rounding of the normal codes that are in it; and what a score owes to
+// its block's scale is one factor for 32 tokens.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels.h"
+
+namespace svdq {
+
+constexpr int kKvBlock = 32;                     // tokens with one scale
+constexpr uint32_t kKvNaN = 0x7fu;               // the NaN code
+
+typedef _Float16 kv_f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 kv_f16x8 __attribute__((ext_vector_type(8)));
+typedef float kv_floatx2 __attribute__((ext_vector_type(2)));
+typedef float kv_floatx4 __attribute__((ext_vector_type(4)));
+typedef float kv_floatx16 __attribute__((ext_vector_type(16)));
+typedef __bf16 kv_bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t kv_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t kv_u32x2 __attribute__((ext_vector_type(2)));
+
+// tokens of slot g: kv_slot_token(g) + {0, 1, 2, 3, 8, 9, 10, 11}
+__host__ __device__ constexpr int kv_slot_token(int g) { return 16 * (g >> 1) + 4 * (g & 1); }
+
+// ---- work items of a ragged batch -----------------------------------------------------------------------------------------
+// Sequence b owns the items from floor(cu[b] / UNIT) + EXTRA b on: room for ceil(n / UNIT) items (EXTRA = 1), or for the aligned units that n
+// tokens from any position on touch (EXTRA = 2), for any lengths, so a grid of floor(T / UNIT) + EXTRA B items is enough without the lengths
+// on the host.  All lanes look at once: 64 sequences a round.  cu is taken as far as it ascends within 0 .. T.
+template <int EXTRA, int UNIT>
+__device__ __forceinline__ int kv_item_sequence(const int32_t *cu, int sequences, int total, int mul, int item, int &local) {
+    const int lane = threadIdx.x & 63;
+    int count = 0;
+    for (int b0 = 0; b0 < sequences; b0 += 64) {
+        const int b = b0 + lane;
+        bool owns = false;
+        if (b < sequences) {
+            int at = cu[b];
+            at = at < 0 ? 0 : at > total ? total : at;
+            owns = (int)((long long)at * mul / UNIT) + EXTRA * b <= item;
+        }
+        const unsigned long long set = __builtin_amdgcn_ballot_w64(owns);
+        count += __builtin_popcountll(set);
+        if (set != ~0ull) break;
+    }
+    const int b = count > 0 ? count - 1 : 0;
+    int at = cu[b];
+    at = at < 0 ? 0 : at > total ? total : at;
+    local = item - ((int)((long long)at * mul / UNIT) + EXTRA * b);
+    return __builtin_amdgcn_readfirstlane(b);
+}
+// sequence b's tokens within 0 .. total
+__device__ __forceinline__ void kv_range(const int32_t *cu, int b, int total, int &first, int &count) {
+    int lo = cu[b], hi = cu[b + 1];
+    lo = lo < 0 ? 0 : lo > total ? total : lo;
+    hi = hi < lo ? lo : hi > total ? total : hi;
+    first = __builtin_amdgcn_readfirstlane(lo);
+    count = __builtin_amdgcn_readfirstlane(hi - lo);
+}
+// tokens of sequence b that the cache can hold
+__device__ __forceinline__ int kv_length(const KvCache &c, const KvBatch &t, int b) {
+    int len = t.kv_len[b];
+    const long long most = (long long)t.table_width << c.page_shift;
+    len = len < 0 ? 0 : (long long)len > most ? (int)most : len;
+    return __builtin_amdgcn_readfirstlane(len);
+}
+// (page, head, block within the page) of block `blk` of sequence b as an index of the scale arrays, -1 where the table names no page of the cache
+__device__ __forceinline__ long long kv_unit(const KvCache &c, const int32_t *table, int width, int b, int head, int blk) {
+    const int bs = c.page_shift - 5;
+    const int page = table[(size_t)b * width + (blk >> bs)];
+    if ((uint32_t)page >= (uint32_t)c.pages) return -1;
+    return (((long long)page * c.heads + head) << bs) + (blk & ((1 << bs) - 1));
+}
+
+// ---- E4M3 -------------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float kv_pow2(int e) {      // 2^e, 0 below the smallest normal number
+    return e < -126 ? 0.f : __uint_as_float((uint32_t)(e + 127) << 23);
+}
+// the byte of the smallest power of two s >= 2^-126 with amax <= 448 s = 1.75 * 2^8 s, from the bits of a finite maximum
+__device__ __forceinline__ int kv_scale_byte(uint32_t amax_bits) {
+    const int byte = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return amax_bits == 0u ? 0 : byte < 1 ? 1 : byte;
+}
+// four numbers of at most 448 in magnitude as four codes, round to nearest even
+__device__ __forceinline__ uint32_t kv_codes4(float a, float b, float c, float d) {
+    int w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+// four codes of a block whose scale grew by 2^-e
+__device__ __forceinline__ uint32_t kv_rescale4(uint32_t w, float factor) {
+    const kv_floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    return kv_codes4(lo[0] * factor, lo[1] * factor, hi[0] * factor, hi[1] * factor);
+}
+// eight codes times a power of two as f16 (exact within its range)
+__device__ __forceinline__ kv_f16x8 kv_f16_of(uint32_t lo, uint32_t hi, float scale) {
+    const kv_f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true);
+    const kv_f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true);
+    return kv_f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// ---- rotation ---------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void kv_floats(uint4 w, float (&x)[8]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void kv_load8(const float *p, float (&x)[8]) {
+    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+// Two channels of a pair: (a, b) -> (a c - b s, b c + a s), each product and the sum rounded once (the build contracts nothing).
+__device__ __forceinline__ float kv_turn_a(float a, float b, float c, float s) { return a * c - b * s; }
+__device__ __forceinline__ float kv_turn_b(float a, float b, float c, float s) { return b * c + a * s; }
+
+// Channels d .. d + 7 (d a multiple of 8) of one row of 16-bit queries at position `pos`, rotated, in fp32.  In the order of halves the partners of
+// eight neighbours are eight neighbours, in the interleaved order they are among themselves (rope_dims is a multiple of 16).
+__device__ __forceinline__ void kv_rotated8(const uint16_t *row, const KvRope &rope, int pos, int d, float (&x)[8]) {
+    kv_floats(*reinterpret_cast<const uint4 *>(row + d), x);
+    if (d >= rope.dims) return;
+    const float *t = rope.table + (size_t)(pos < 0 ? 0 : pos < rope.positions ? pos : rope.positions - 1) * rope.dims;
+    const int half = rope.dims / 2;
+    if (rope.interleaved) {
+        const float4 c4 = *reinterpret_cast<const float4 *>(t + d / 2), s4 = *reinterpret_cast<const float4 *>(t + half + d / 2);
+        const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = x[2 * i], b = x[2 * i + 1];
+            x[2 * i] = kv_turn_a(a, b, c[i], s[i]);
+            x[2 * i + 1] = kv_turn_b(a, b, c[i], s[i]);
+        }
+        return;
+    }
+    const bool second = d >= half;
+    const int i0 = second ? d - half : d;
+    float y[8], c[8], s[8];
+    kv_floats(*reinterpret_cast<const uint4 *>(row + (second ? d - half : d + half)), y);
+    kv_load8(t + i0, c);
+    kv_load8(t + half + i0, s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = second ? kv_turn_b(y[i], x[i], c[i], s[i]) : kv_turn_a(x[i], y[i], c[i], s[i]);
+}
+
+// ---- reductions over the lane groups of a wavefront: every lane gets the result (v_permlane32_swap / v_permlane16_swap of a register with itself
+// leaves one operand of each pair of halves, or of rows, in both) -------------------------------------------------------------
+__device__ __forceinline__ void kv_swap32(float x, float &a, float &b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    a = __uint_as_float(r[0]);
+    b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ void kv_swap16(float x, float &a, float &b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    a = __uint_as_float(r[0]);
+    b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float kv_max32(float x) { float a, b; kv_swap32(x, a, b); return fmaxf(a, b); }
+__device__ __forceinline__ float kv_max16(float x) { float a, b; kv_swap16(x, a, b); return fmaxf(a, b); }
+__device__ __forceinline__ float kv_sum32(float x) { float a, b; kv_swap32(x, a, b); return a + b; }
+__device__ __forceinline__ float kv_sum16(float x) { float a, b; kv_swap16(x, a, b); return a + b; }
+
+}  // namespace svdq

@@ -767,4 +767,41 @@ inline Workspace workspace_layout(int M, int K, int N, int rank, int ksplit_over
     return w;
 }
 
+// ---- attention over the paged 8-bit cache: which kernel, and how the keys are cut --------------------------------------------------------
+constexpr int kKvTileRows = 128;
+constexpr unsigned long long kKvArrived = 0x4b56535644514152ull;      // as kActArrived: what a workgroup leaves in its arrival word
+// Rows of a sequence and key head up to which the kernel of few rows takes a launch (sixteen rows a workgroup; it reads the keys once per sixteen).
+constexpr int kKvFewRows = 32;
+struct KvPlan {
+    bool few;
+    int row_tiles, chunk_blocks, chunks;
+    size_t parts_off, ml_off, words_off, total;      // bytes of the workspace
+};
+inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len) {
+    KvPlan p{};
+    const long long rows = (long long)max_new * group;
+    p.few = rows <= kKvFewRows;
+    p.row_tiles = p.few ? (int)((rows + 15) / 16) : 0;
+    p.chunks = 1;
+    const int blocks = (max_len + 31) / 32 > 0 ? (max_len + 31) / 32 : 1;
+    p.chunk_blocks = blocks;
+    if (p.few) {
+        const long long wgs = (long long)sequences * heads * (p.row_tiles > 0 ? p.row_tiles : 1);
+        long long want = (1024 + wgs - 1) / wgs;                             // about four workgroups per CU
+        if (want > (blocks + 7) / 8) want = (blocks + 7) / 8;                // two blocks a wavefront at least
+        p.chunk_blocks = (int)((blocks + want - 1) / want);
+        if (p.chunk_blocks > 64) p.chunk_blocks = 64;                        // long sequences of a ragged batch in pieces of 2048 tokens
+        p.chunks = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
+    }
+    p.total = 256;
+    if (p.chunks > 1) {
+        const size_t parts = (size_t)sequences * p.row_tiles * heads * p.chunks;
+        p.parts_off = 0;
+        p.ml_off = align256(parts * 16 * dim * 4);
+        p.words_off = p.ml_off + align256(parts * 16 * 2 * 4);
+        p.total = p.words_off + align256(parts * 8);
+    }
+    return p;
+}
+
 }  // namespace svdq

@@ -31,6 +31,7 @@ EXPORTS = [
     "svdq_workspace_bytes", "svdq_linear_forward", "svdq_debug_act", "svdq_debug_group_acc",
     "svdq_forward_options", "svdq_profile_event", "svdq_mfma_peak_probe", "svdq_linear_forward_static",
     "svdq_debug_launch_plan",
+    "svdq_kv_cache_sizes", "svdq_kv_append", "svdq_kv_attention_workspace_bytes", "svdq_kv_attention", "svdq_kv_gather",
 ]
 
 
@@ -48,6 +49,30 @@ class Sizes(C.Structure):
 
 class LayerDev(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("rinv", "l1s", "l2", "wcodes", "wscales", "bias")] + [("shape", Shape)]
+
+
+class KVShape(C.Structure):
+    _fields_ = [("kv_heads", C.c_int), ("head_dim", C.c_int), ("page_tokens", C.c_int)]
+
+
+class KVSizes(C.Structure):
+    _fields_ = [("codes", C.c_size_t), ("scales", C.c_size_t)]
+
+
+class KVCacheDev(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales")] + [("pages", C.c_int), ("shape", KVShape)]
+
+
+class KVBatchDev(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("cu_new", "kv_len", "block_table")] + [(n, C.c_int) for n in ("sequences", "table_width", "new_tokens", "max_new", "max_len")]
+
+
+class KVRopeDev(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("positions", C.c_int), ("dims", C.c_int), ("interleaved", C.c_int)]
+
+
+class KVRowsDev(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 _lib = None
@@ -104,6 +129,13 @@ def lib() -> C.CDLL:
         L.svdq_forward_options.argtypes = [C.c_int]
         L.svdq_profile_event.argtypes = [vp]
         L.svdq_mfma_peak_probe.argtypes = [C.c_int, C.c_int, vp, C.c_size_t, vp, C.POINTER(C.c_double)]
+        L.svdq_kv_cache_sizes.argtypes = [C.POINTER(KVShape), C.c_int, C.POINTER(KVSizes)]
+        L.svdq_kv_append.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), C.POINTER(KVRopeDev), C.POINTER(KVRowsDev), C.POINTER(KVRowsDev), vp]
+        L.svdq_kv_attention_workspace_bytes.restype = C.c_size_t
+        L.svdq_kv_attention_workspace_bytes.argtypes = [C.POINTER(KVShape)] + [C.c_int] * 4
+        L.svdq_kv_attention.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), C.POINTER(KVRopeDev), C.POINTER(KVRowsDev), C.c_int, C.c_float, C.c_int, C.c_int,
+                                        vp, vp, C.c_size_t, vp]
+        L.svdq_kv_gather.argtypes = [C.POINTER(KVCacheDev), vp, vp, vp, C.c_int, C.c_int, C.c_int, vp, vp, vp]
         _lib = L
     return _lib
 
