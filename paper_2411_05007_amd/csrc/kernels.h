@@ -245,9 +245,9 @@ struct KvAttentionParams {
     float scale;             // of the scores, times log2(e)
     int causal, window;      // window = 0: none
     int row_tiles;           // few-row kernel: tiles of 16 rows a sequence and head may need
+    int row_cap;             // few-row kernel: rows that a tile can have
     int chunk_blocks, chunks;      // few-row kernel: the keys are cut into chunks of chunk_blocks blocks (the last takes the rest)
-    float *partial;          // chunks > 1: fp32 [sequence][row tile][head][chunk][16][dim], then maxima and sums [...][16][2]
-    float *partial_ml;
+    float *partial;          // chunks > 1: fp32 [sequence][row tile][head][chunk]([row_cap][dim] sums, [row_cap][2] maximum and sum of weights)
     unsigned long long *arrived;      // chunks > 1: [sequence][row tile][head][chunk]
 };
 hipError_t launch_kv_attention_rows(const KvAttentionParams &p, hipStream_t stream);      // few rows (kv_rows_kernel.hip)

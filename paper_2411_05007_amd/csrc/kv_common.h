@@ -126,32 +126,75 @@ __device__ __forceinline__ void kv_load8(const float *p, float (&x)[8]) {
 __device__ __forceinline__ float kv_turn_a(float a, float b, float c, float s) { return a * c - b * s; }
 __device__ __forceinline__ float kv_turn_b(float a, float b, float c, float s) { return b * c + a * s; }
 
-// Channels d .. d + 7 (d a multiple of 8) of one row of 16-bit queries at position `pos`, rotated, in fp32.  In the order of halves the partners of
-// eight neighbours are eight neighbours, in the interleaved order they are among themselves (rope_dims is a multiple of 16).
-__device__ __forceinline__ void kv_rotated8(const uint16_t *row, const KvRope &rope, int pos, int d, float (&x)[8]) {
-    kv_floats(*reinterpret_cast<const uint4 *>(row + d), x);
-    if (d >= rope.dims) return;
-    const float *t = rope.table + (size_t)(pos < 0 ? 0 : pos < rope.positions ? pos : rope.positions - 1) * rope.dims;
-    const int half = rope.dims / 2;
-    if (rope.interleaved) {
-        const float4 c4 = *reinterpret_cast<const float4 *>(t + d / 2), s4 = *reinterpret_cast<const float4 *>(t + half + d / 2);
-        const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+// Eight channels at each of N places of one row of 16-bit queries at position `pos`, rotated, in fp32; place(i) is a multiple of 8.  In the order of halves
+// the partners of eight neighbours are eight neighbours, in the interleaved order they are among themselves (dims is a multiple of 16).  Everything
+// is requested before the first is used; channels past `dims` are loaded like the others and left as they are.
+template <int N>
+struct KvRotating {
+    uint4 own[N], other[N];
+    float c[N][8], s[N][8];
+    template <typename Place>
+    __device__ __forceinline__ void request(const uint16_t *row, const KvRope &rope, int pos, Place place) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float a = x[2 * i], b = x[2 * i + 1];
-            x[2 * i] = kv_turn_a(a, b, c[i], s[i]);
-            x[2 * i + 1] = kv_turn_b(a, b, c[i], s[i]);
+        for (int i = 0; i < N; ++i) own[i] = *reinterpret_cast<const uint4 *>(row + place(i));
+        if (rope.dims == 0) return;
+        const float *t = rope.table + (size_t)(pos < 0 ? 0 : pos < rope.positions ? pos : rope.positions - 1) * rope.dims;
+        const int half = rope.dims / 2;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int d = place(i) < rope.dims ? place(i) : 0;
+            const int first = rope.interleaved ? d / 2 : d >= half ? d - half : d;
+            other[i] = own[i];
+            if (!rope.interleaved) other[i] = *reinterpret_cast<const uint4 *>(row + (d >= half ? d - half : d + half));
+            // (interleaved: the first four of each)
+            const float4 c0 = *reinterpret_cast<const float4 *>(t + first), s0 = *reinterpret_cast<const float4 *>(t + half + first);
+            const int more = rope.interleaved ? 0 : 4;
+            const float4 c1 = *reinterpret_cast<const float4 *>(t + first + more), s1 = *reinterpret_cast<const float4 *>(t + half + first + more);
+            c[i][0] = c0.x; c[i][1] = c0.y; c[i][2] = c0.z; c[i][3] = c0.w; c[i][4] = c1.x; c[i][5] = c1.y; c[i][6] = c1.z; c[i][7] = c1.w;
+            s[i][0] = s0.x; s[i][1] = s0.y; s[i][2] = s0.z; s[i][3] = s0.w; s[i][4] = s1.x; s[i][5] = s1.y; s[i][6] = s1.z; s[i][7] = s1.w;
         }
-        return;
     }
-    const bool second = d >= half;
-    const int i0 = second ? d - half : d;
-    float y[8], c[8], s[8];
-    kv_floats(*reinterpret_cast<const uint4 *>(row + (second ? d - half : d + half)), y);
-    kv_load8(t + i0, c);
-    kv_load8(t + half + i0, s);
+    template <typename Place>
+    __device__ __forceinline__ void finish(const KvRope &rope, Place place, float (&x)[N][8]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = second ? kv_turn_b(y[i], x[i], c[i], s[i]) : kv_turn_a(x[i], y[i], c[i], s[i]);
+        for (int i = 0; i < N; ++i) kv_floats(own[i], x[i]);
+        if (rope.dims == 0) return;
+        if (rope.interleaved) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const bool turn = place(i) < rope.dims;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = x[i][2 * e], b = x[i][2 * e + 1];
+                    x[i][2 * e] = turn ? kv_turn_a(a, b, c[i][e], s[i][e]) : a;
+                    x[i][2 * e + 1] = turn ? kv_turn_b(a, b, c[i][e], s[i][e]) : b;
+                }
+            }
+            return;
+        }
+        const int half = rope.dims / 2;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float y[8];
+            kv_floats(other[i], y);
+            const bool turn = place(i) < rope.dims, second = place(i) >= half;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float z = second ? kv_turn_b(y[e], x[i][e], c[i][e], s[i][e]) : kv_turn_a(x[i][e], y[e], c[i][e], s[i][e]);
+                x[i][e] = turn ? z : x[i][e];
+            }
+        }
+    }
+};
+template <int N, typename Place>
+__device__ __forceinline__ void kv_rotated(const uint16_t *row, const KvRope &rope, int pos, Place place, float (&x)[N][8]) {
+    KvRotating<N> t;
+    t.request(row, rope, pos, place);
+    t.finish(rope, place, x);
+}
+// Barrier of a workgroup for what its wavefronts wrote to LDS: loads from memory stay in flight.
+__device__ __forceinline__ void kv_lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // ---- reductions over the lane groups of a wavefront: every lane gets the result (v_permlane32_swap / v_permlane16_swap of a register with itself

@@ -9,33 +9,48 @@
 // O^T += V^T P^T with the values as code * 2^(byte - reference), exact, the reference exponent the largest seen.  P is scaled by 2^8 (and may reach 2^14
 // before the maximum is renewed), so that f16 keeps eleven bits of weights down to 2^-22 of the largest; f16 for Q, scaled by a power of two per
 // row, for the same eleven bits.
-// The wavefronts' sums meet in LDS.  With several chunks the parts lie in the workspace and the workgroup that finds all of its row tile arrived adds
-// them in chunk order (the same bits whoever it is).
-// Bound: memory, one byte per channel of a key and a value.
+// Loads: the pages and scale bytes of a wavefront's next 64 blocks are looked up at once, one in a lane; the codes of two blocks are in flight (16 KB a
+// wavefront, three workgroups a CU), each requested right behind the last use of its registers.
+// The wavefronts' sums meet in LDS.  With several chunks the parts lie in the workspace, past the L2s, and the workgroup that finds all of its row tile
+// arrived adds them in chunk order (the same bits whoever it is), eight requests in flight a thread; nothing waits for another workgroup.
+// Bound: memory, one byte per channel of a key and a value: one sequence of 131071 keys, 8 key heads of 128, 32 query heads 54 us (5.0 TB/s), 64 sequences
+// of 100 to 16384 keys 255 us (4.5 TB/s).  Short ones by a chain of round trips: 5.7 us for one block (lengths, table, codes, queries turned on the way), 9.5 us for 777 keys of eight
+// heads, where the eight CUs draw 52 GB/s each.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "buffer.h"
 #include "kernels.h"
 #include "kv_common.h"
 #include "layout.h"
+#include "lds_limit.h"
 
 namespace svdq {
 namespace {
 
 constexpr float kNone = -1e30f;                  // the running maximum before the first key
 constexpr float kShift = 8.f, kSlack = 6.f;      // P is exp2(t - m + kShift); m is renewed when a score passes it by kSlack
-constexpr int kWaves = 4;
+constexpr int WAVES = 4;
 
 template <int D>
-struct Block { uint4 k[2][D / 64]; uint4 v[D / 32]; uint32_t kb, vb; };      // 32 tokens of a head, as a lane holds them
+struct Block { uint4 k[2][D / 64]; uint4 v[D / 32]; };      // 32 tokens of a head, as a lane holds them
+
+// floats of a row in LDS, and the bytes of a workgroup's LDS: first the queries as operands in fp32 and maxima per wavefront, then [wave][row][row_floats], then maximum and sum [wave][16][2], then the reference exponents
+constexpr int row_floats(int D) { return D + 4; }
+// or, where parts meet: weights [chunk][row], a factor per row, 16 bytes a thread
+constexpr int rows_lds_bytes(int D, int waves, int cap, int chunks) {
+    const int loop = (waves * cap * row_floats(D) + waves * 32 + waves) * 4, queries = (D / 32 * 512 + waves * 64) * 4, parts = chunks > 1 ? (chunks * cap + cap + 8) * 4 + waves * 64 * 16 : 0;
+    return loop > parts ? loop > queries ? loop : queries : parts > queries ? parts : queries;
+}
+constexpr int kAgent = 16;      // cache policy of a buffer access that all XCDs see
 
 template <int D>
-__global__ __launch_bounds__(kWaves * 64) void kv_rows_kernel(KvAttentionParams p) {
+__global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_rows_kernel(KvAttentionParams p) {
     constexpr int C = D / 32;                    // runs of 32 channels = steps of K Q^T per 16 tokens
-    constexpr int kRow = D + 4;                  // floats of a row in LDS
-    __shared__ __attribute__((aligned(16))) float sums[kWaves][16][kRow];
-    __shared__ float ml[kWaves][16][2];
-    __shared__ float refs[kWaves];
+    constexpr int kRow = row_floats(D);
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const int cap = p.row_cap;                   // rows that a tile can have
+    float *sums = lds, *ml = lds + WAVES * cap * kRow, *refs = ml + WAVES * 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, q4 = lane >> 4;
     const int head = blockIdx.y, b = blockIdx.z / p.row_tiles, tile = blockIdx.z % p.row_tiles;
@@ -63,58 +78,88 @@ __global__ __launch_bounds__(kWaves * 64) void kv_rows_kernel(KvAttentionParams 
 
     const int32_t *table = p.batch.table + (size_t)b * p.batch.table_width;
     const int bs = p.cache.page_shift - 5;
-    auto unit_of = [&](int blk) {      // blk in [c0, c1)
-        const int page = table[blk >> bs];
-        return (uint32_t)page < (uint32_t)p.cache.pages ? (((long long)page * p.cache.heads + head) << bs) + (blk & ((1 << bs) - 1)) : -1ll;
+    // The wavefront's blocks c0 + wave + WAVES i: their pages and scale bytes, 64 blocks at a time, one in a lane
+    int base = c0 + wave, left = base < c1 ? (c1 - base + WAVES - 1) / WAVES : 0, here = 0, page_l = -1, kb_l = 0, vb_l = 0;
+    auto look_up = [&]() {
+        here = left < 64 ? left : 64;
+        page_l = here == 0 ? -1 : table[(base + WAVES * (lane < here ? lane : 0)) >> bs];
     };
-    auto load = [&](long long unit) {
-        Block<D> t;
-        const size_t u = unit < 0 ? 0 : (size_t)unit;      // (a block that the table does not name is masked)
+    auto look_up_bytes = [&]() {
+        const int blk = base + WAVES * lane;
+        const bool named = lane < here && (uint32_t)page_l < (uint32_t)p.cache.pages;
+        const size_t u = named ? (((size_t)page_l * p.cache.heads + head) << bs) + (blk & ((1 << bs) - 1)) : 0;
+        page_l = named ? page_l : -1;
+        kb_l = p.cache.ks[u];
+        vb_l = p.cache.vs[u];
+    };
+    const uint32_t k_off = (uint32_t)((16 * (l16 >> 3) + (l16 & 7)) * D + 16 * q4), v_off = (uint32_t)((l16 * 4 + q4) * 16);
+    // Block i of the wavefront.  Past the last one, or where the table names no page, every lane reads the first 16 bytes of the cache: loads are issued
+    // whether they are needed or not, so that a wait for one block leaves the next ones in flight.
+    auto load = [&](Block<D> &t, int i) {
+        const int page = __builtin_amdgcn_readlane(page_l, i < here ? i : 0);
+        const bool real = i < here && page >= 0;
+        const size_t u = real ? (((size_t)page * p.cache.heads + head) << bs) + ((base + WAVES * i) & ((1 << bs) - 1)) : 0;
         const uint8_t *k = p.cache.k + u * (32 * D), *v = p.cache.v + u * (32 * D);
-        t.kb = p.cache.ks[u];
-        t.vb = p.cache.vs[u];
+        const uint32_t ko = real ? k_off : 0u, vo = real ? v_off : 0u;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = 16 * (l16 >> 3) + 8 * i + (l16 & 7);
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) t.k[i][c] = *reinterpret_cast<const uint4 *>(k + row * D + 64 * c + 16 * q4);
-        }
+            for (int c = 0; c < D / 64; ++c) t.k[j][c] = *reinterpret_cast<const uint4 *>(k + ko + 8 * j * D + 64 * c);
 #pragma unroll
-        for (int a = 0; a < D / 32; ++a) t.v[a] = *reinterpret_cast<const uint4 *>(v + ((a * 16 + l16) * 4 + q4) * 16);
-        return t;
+        for (int a = 0; a < D / 32; ++a) t.v[a] = *reinterpret_cast<const uint4 *>(v + vo + 1024 * a);
     };
-    int blk = c0 + wave;
-    long long unit = -1;
-    Block<D> cur;
-    if (blk < c1) {
-        unit = unit_of(blk);
-        cur = load(unit);
-    }
-
-    // the queries: f16 of the rotated row times a power of two that brings its largest element to [2^14, 2^15)
+    look_up();
+    // The queries, a step of the wavefronts each: requested before the blocks, whose addresses wait for the table
+    constexpr int kMine = (C + WAVES - 1) / WAVES;      // steps of a wavefront (D = 64: of the first two)
+    const auto place = [&](int i) {                     // step c: channels 64 (c / 2) + 16 q4 + 8 (c % 2) .. + 7
+        const int c = wave * kMine + i < C ? wave * kMine + i : C - 1;
+        return 64 * (c / 2) + 16 * q4 + 8 * (c % 2);
+    };
+    KvRotating<kMine> turning;
+    turning.request(p.q.data + (size_t)(t0 + tok) * p.q.token_stride + qh * p.q.head_stride, p.rope, pos, place);
+    __builtin_amdgcn_sched_barrier(0);
+    look_up_bytes();
+    Block<D> even, odd;
+    load(even, 0);
+    load(odd, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    // f16 of the rotated row times a power of two that brings its largest element to [2^14, 2^15)
     kv_f16x8 qf[C];
     float to_t;      // score -> exponent of 2, but for the block's scale
     {
-        const uint16_t *row = p.q.data + (size_t)(t0 + tok) * p.q.token_stride + qh * p.q.head_stride;
-        float x[C][8];
+        float x[kMine][8];
+        turning.finish(p.rope, place, x);
         uint32_t top = 0u;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {      // step c: channels 64 (c / 2) + 16 q4 + 8 (c % 2) .. + 7
-            kv_rotated8(row, p.rope, pos, 64 * (c / 2) + 16 * q4 + 8 * (c % 2), x[c]);
+        for (int i = 0; i < kMine; ++i) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const uint32_t u = __float_as_uint(x[c][e]) & 0x7fffffffu;
+                const uint32_t u = __float_as_uint(x[i][e]) & 0x7fffffffu;
                 top = top > u ? top : u;
             }
+            if (wave * kMine + i < C) {
+                float *dst = lds + ((wave * kMine + i) * 64 + lane) * 8;
+                *reinterpret_cast<kv_floatx4 *>(dst) = kv_floatx4{x[i][0], x[i][1], x[i][2], x[i][3]};
+                *reinterpret_cast<kv_floatx4 *>(dst + 4) = kv_floatx4{x[i][4], x[i][5], x[i][6], x[i][7]};
+            }
         }
-        const float m = kv_max32(kv_max16(__uint_as_float(top >= 0x7f800000u ? 0x7f800000u : top)));
+        lds[C * 512 + wave * 64 + lane] = kv_max32(kv_max16(__uint_as_float(top >= 0x7f800000u ? 0x7f800000u : top)));
+        kv_lds_barrier();
+        float m = lds[C * 512 + lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, lds[C * 512 + w * 64 + lane]);
         const int e = (int)(__float_as_uint(m) >> 23) - 127;                          // m in [2^e, 2^(e + 1))
         const int up = e < -100 ? 114 : e > 127 ? 0 : 14 - e;                         // (not finite: as it is, the row becomes NaN)
         const float f = kv_pow2(up);
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c) {
+            const kv_floatx4 lo = *reinterpret_cast<const kv_floatx4 *>(lds + (c * 64 + lane) * 8), hi = *reinterpret_cast<const kv_floatx4 *>(lds + (c * 64 + lane) * 8 + 4);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) qf[c][i] = (_Float16)(x[c][i] * f);
+            for (int i = 0; i < 4; ++i) {
+                qf[c][i] = (_Float16)(lo[i] * f);
+                qf[c][4 + i] = (_Float16)(hi[i] * f);
+            }
+        }
         to_t = p.scale * kv_pow2(-up);
     }
 
@@ -122,38 +167,35 @@ __global__ __launch_bounds__(kWaves * 64) void kv_rows_kernel(KvAttentionParams 
     float m = kNone, l = 0.f;
     int ref = 0;                                 // byte of the reference scale of the values in o
 
-    for (; blk < c1; blk += kWaves) {
-        Block<D> nxt;
-        const int after = blk + kWaves;
-        long long unit_next = -1;
-        if (after < c1) {
-            unit_next = unit_of(after);
-            nxt = load(unit_next);
-        }
-        const int kb = __builtin_amdgcn_readfirstlane((int)cur.kb), vb = __builtin_amdgcn_readfirstlane((int)cur.vb);
+    auto step = [&](Block<D> &cur, int i) {
+        const int blk = base + WAVES * i, kb = __builtin_amdgcn_readlane(kb_l, i), vb = __builtin_amdgcn_readlane(vb_l, i);
+        const bool named = __builtin_amdgcn_readlane(page_l, i) >= 0;
         kv_floatx4 s[2] = {};
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int c = 0; c < D / 64; ++c)
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) {
-                s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(cur.k[i][c].x, cur.k[i][c].y, 1.f), qf[2 * c], s[i], 0, 0, 0);
-                s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(cur.k[i][c].z, cur.k[i][c].w, 1.f), qf[2 * c + 1], s[i], 0, 0, 0);
+            for (int j = 0; j < 2; ++j) {
+                s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(cur.k[j][c].x, cur.k[j][c].y, 1.f), qf[2 * c], s[j], 0, 0, 0);
+                s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(cur.k[j][c].z, cur.k[j][c].w, 1.f), qf[2 * c + 1], s[j], 0, 0, 0);
             }
         // the lane's eight tokens are those of slot q4
         const float f = to_t * kv_pow2(kb - 127);
         float t[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) t[j] = s[j / 4][j % 4] * f;
-        const bool edge = unit < 0 || blk * kKvBlock < all_lo || blk * kKvBlock + kKvBlock > all_hi;
-        uint32_t live[2] = {~0u, ~0u};           // bytes of the codes of tokens that exist
-        if (edge) {
+        if (!named || blk * kKvBlock < all_lo || blk * kKvBlock + kKvBlock > all_hi) {
             const int first = blk * kKvBlock + kv_slot_token(q4);
+            uint32_t live[2] = {~0u, ~0u};       // bytes of the codes of tokens that exist
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int key = first + (j & 3) + 8 * (j >> 2);
-                const bool ok = unit >= 0 && key >= seen_lo && key < seen_hi && key < len;
+                const bool ok = named && key >= seen_lo && key < seen_hi && key < len;
                 t[j] = ok ? t[j] : -__builtin_inff();
-                if (unit < 0 || key >= len) live[j >> 2] &= ~(0xffu << (8 * (j & 3)));
+                if (!named || key >= len) live[j >> 2] &= ~(0xffu << (8 * (j & 3)));
+            }
+#pragma unroll
+            for (int a = 0; a < D / 32; ++a) {
+                cur.v[a].x &= live[0]; cur.v[a].y &= live[1]; cur.v[a].z &= live[0]; cur.v[a].w &= live[1];
             }
         }
         float top = t[0];
@@ -164,7 +206,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_rows_kernel(KvAttentionParams 
         if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0ull || ref_new != ref) {
             const float m_new = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(m - m_new);
             l *= keep;
-            const float both = keep * kv_pow2(ref - ref_new < -126 ? -127 : ref - ref_new);
+            const float both = keep * kv_pow2(ref - ref_new);
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) o[d] *= both;
             m = m_new;
@@ -180,125 +222,189 @@ __global__ __launch_bounds__(kWaves * 64) void kv_rows_kernel(KvAttentionParams 
         const float vf = kv_pow2(vb - ref);
 #pragma unroll
         for (int a = 0; a < D / 32; ++a) {
-            if (edge) {
-                cur.v[a].x &= live[0]; cur.v[a].y &= live[1]; cur.v[a].z &= live[0]; cur.v[a].w &= live[1];
-            }
             o[2 * a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(cur.v[a].x, cur.v[a].y, vf), pf, o[2 * a], 0, 0, 0);
             o[2 * a + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(cur.v[a].z, cur.v[a].w, vf), pf, o[2 * a + 1], 0, 0, 0);
         }
-        cur = nxt;
-        unit = unit_next;
+    };
+    for (;;) {
+        for (int i = 0; i < here; i += 2) {
+            step(even, i);
+            load(even, i + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + 1 < here) step(odd, i + 1);
+            load(odd, i + 3);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        left -= here;
+        if (left <= 0) break;
+        base += WAVES * 64;
+        look_up();
+        look_up_bytes();
+        load(even, 0);
+        load(odd, 1);
     }
 
     // ---- the wavefronts' sums meet ----
+    __syncthreads();      // (the queries lay there)
     l = kv_sum32(kv_sum16(l));
     if (q4 == 0) {
-        ml[wave][l16][0] = m;
-        ml[wave][l16][1] = l;
+        ml[(wave * 16 + l16) * 2] = m;
+        ml[(wave * 16 + l16) * 2 + 1] = l;
     }
     if (lane == 0) refs[wave] = (float)ref;
     __syncthreads();
     {
         float top = kNone, most = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            top = fmaxf(top, ml[w][l16][0]);
+        for (int w = 0; w < WAVES; ++w) {
+            top = fmaxf(top, ml[(w * 16 + l16) * 2]);
             most = fmaxf(most, refs[w]);
         }
         const float f = __builtin_amdgcn_exp2f(m - top) * kv_pow2(ref - (int)most);
+        if (l16 < cap)
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) *reinterpret_cast<kv_floatx4 *>(&sums[wave][l16][16 * d + 4 * q4]) = o[d] * f;
+            for (int d = 0; d < D / 16; ++d) *reinterpret_cast<kv_floatx4 *>(sums + (wave * cap + l16) * kRow + 16 * d + 4 * q4) = o[d] * f;
     }
     __syncthreads();
-    // element (row, d) by thread; the whole block of 16 x D in 16-byte pieces
+    // pieces of four channels of a row
     const long long part = ((long long)blockIdx.z * p.cache.heads + head) * p.chunks;      // of this row tile's parts
-    const int live_rows = rows - tile * 16 < 16 ? rows - tile * 16 : 16;
-    for (int i = threadIdx.x; i < live_rows * (D / 4); i += kWaves * 64) {
+    const int live_rows = rows - tile * 16 < 16 ? rows - tile * 16 : 16, pieces = live_rows * (D / 4);
+    const size_t part_floats = (size_t)cap * (D + 2);      // [cap][D] sums, [cap][2] maximum and sum of weights
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.partial + part * part_floats, (size_t)nchunks * part_floats * 4);
+    auto store = [&](int row, int d, kv_floatx4 x, float inv) {
+        const int rr = tile * 16 + row;
+        uint16_t *dst = p.out + ((size_t)(t0 + rr / p.group) * p.q_heads + head * p.group + rr % p.group) * D + d;
+        const kv_bf16x2 lo = {(__bf16)(x[0] * inv), (__bf16)(x[1] * inv)}, hi = {(__bf16)(x[2] * inv), (__bf16)(x[3] * inv)};
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+    };
+    auto inverse = [](float sum) { return sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum; };      // (no key seen: zeros)
+    for (int i = threadIdx.x; i < pieces; i += WAVES * 64) {
         const int row = i / (D / 4), d = i % (D / 4) * 4;
         float top = kNone, most = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            top = fmaxf(top, ml[w][row][0]);
+        for (int w = 0; w < WAVES; ++w) {
+            top = fmaxf(top, ml[(w * 16 + row) * 2]);
             most = fmaxf(most, refs[w]);
         }
         kv_floatx4 x = {};
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            x += *reinterpret_cast<const kv_floatx4 *>(&sums[w][row][d]);
-            sum += ml[w][row][1] * __builtin_amdgcn_exp2f(ml[w][row][0] - top);
+        for (int w = 0; w < WAVES; ++w) {
+            x += *reinterpret_cast<const kv_floatx4 *>(sums + (w * cap + row) * kRow + d);
+            sum += ml[(w * 16 + row) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(w * 16 + row) * 2] - top);
         }
         x *= kv_pow2((int)most - 127);
         if (nchunks > 1) {      // past the L2 of this XCD: the workgroup that adds the parts may run on another
-            float *dst = p.partial + ((part + chunk) * 16 + row) * D + d;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) __hip_atomic_store(dst + k, x[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (d == 0) {
-                float *q = p.partial_ml + ((part + chunk) * 16 + row) * 2;
-                __hip_atomic_store(q, top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __hip_atomic_store(q + 1, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
+            const int at = (int)(chunk * part_floats * 4);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(kv_u32x4, x), rs, at + (row * D + d) * 4, 0, kAgent);
+            if (d == 0) __builtin_amdgcn_raw_buffer_store_b64(kv_u32x2{__float_as_uint(top), __float_as_uint(sum)}, rs, at + (cap * D + row * 2) * 4, 0, kAgent);
         } else {
-            const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;      // (no key seen: zeros)
-            const int rr = tile * 16 + row;
-            uint16_t *dst = p.out + ((size_t)(t0 + rr / p.group) * p.q_heads + head * p.group + rr % p.group) * D + d;
-            const kv_bf16x2 lo = {(__bf16)(x[0] * inv), (__bf16)(x[1] * inv)}, hi = {(__bf16)(x[2] * inv), (__bf16)(x[3] * inv)};
-            *reinterpret_cast<uint2 *>(dst) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+            store(row, d, x, inverse(sum));
         }
     }
     if (nchunks == 1) return;
 
     // ---- the parts of the row tile meet: the arrival words hold anything but kKvArrived until a workgroup marks its own, and are cleared at the end ----
-    __shared__ int everyone;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x == 0) everyone = 1;
+    __shared__ int missing;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's stores are acknowledged
+    if (threadIdx.x == 0) missing = 0;
     __syncthreads();
     unsigned long long *words = p.arrived + part;
-    if (threadIdx.x == 0) {
-        (void)__hip_atomic_exchange(words + chunk, kKvArrived, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    if (wave == 0) {
+        if (lane == 0) (void)__hip_atomic_exchange(words + chunk, kKvArrived, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        bool all = true;
+        for (int i = lane; i < nchunks; i += 64) all = all && __hip_atomic_load(words + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == kKvArrived;
+        if (__builtin_amdgcn_ballot_w64(!all) != 0ull && lane == 0) missing = 1;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < nchunks; i += kWaves * 64)
-        if (__hip_atomic_load(words + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != kKvArrived) everyone = 0;
-    __syncthreads();
-    if (!everyone) return;
-    for (int i = threadIdx.x; i < live_rows * (D / 4); i += kWaves * 64) {
-        const int row = i / (D / 4), d = i % (D / 4) * 4;
-        float top = kNone, sum = 0.f;
-        kv_floatx4 x = {};
-        for (int c = 0; c < nchunks; ++c) {
-            const float *q = p.partial_ml + ((part + c) * 16 + row) * 2, *src = p.partial + ((part + c) * 16 + row) * D + d;
-            const float mc = __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), lc = __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            kv_floatx4 y;
+    if (missing) return;
+    // weights of the parts, [chunk][row], then 1 / their sum per row; thread groups add every so many parts, and the groups meet in LDS
+    float *weight = lds, *inv_of = weight + nchunks * cap, *meet = inv_of + ((cap + 3) & ~3);
+    meet = lds + (((meet - lds) + 3) & ~3);
+    for (int row = wave; row < live_rows; row += WAVES) {
+        float mx = kNone, part_m[kKvMostChunks / 64], part_l[kKvMostChunks / 64];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = __hip_atomic_load(src + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const float m_new = fmaxf(top, mc), f = __builtin_amdgcn_exp2f(top - m_new), g = __builtin_amdgcn_exp2f(mc - m_new);
-            x = x * f + y * g;
-            sum = sum * f + lc * g;
-            top = m_new;
+        for (int k = 0; k < kKvMostChunks / 64; ++k) {
+            const int c = lane + 64 * k;
+            kv_u32x2 w = {__float_as_uint(kNone), 0u};
+            if (c < nchunks) w = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)((c * part_floats + cap * D + row * 2) * 4), 0, kAgent);
+            part_m[k] = __uint_as_float(w[0]);
+            part_l[k] = __uint_as_float(w[1]);
+            mx = fmaxf(mx, part_m[k]);
         }
-        const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
-        const int rr = tile * 16 + row;
-        uint16_t *dst = p.out + ((size_t)(t0 + rr / p.group) * p.q_heads + head * p.group + rr % p.group) * D + d;
-        const kv_bf16x2 lo = {(__bf16)(x[0] * inv), (__bf16)(x[1] * inv)}, hi = {(__bf16)(x[2] * inv), (__bf16)(x[3] * inv)};
-        *reinterpret_cast<uint2 *>(dst) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) mx = fmaxf(mx, __shfl_xor(mx, s));
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < kKvMostChunks / 64; ++k) {
+            const int c = lane + 64 * k;
+            const float f = __builtin_amdgcn_exp2f(part_m[k] - mx);
+            sum += part_l[k] * f;
+            if (c < nchunks) weight[c * cap + row] = f;
+        }
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) sum += __shfl_xor(sum, s);
+        if (lane == 0) inv_of[row] = inverse(sum);
+    }
+    __syncthreads();
+    const int groups = pieces < WAVES * 64 ? WAVES * 64 / pieces : 1, mine = threadIdx.x / pieces;
+    for (int i0 = 0; i0 < pieces; i0 += WAVES * 64) {      // (more than one round: one group)
+        const int i = groups > 1 ? threadIdx.x % pieces : i0 + threadIdx.x, row = i / (D / 4), d = i % (D / 4) * 4;
+        const bool works = groups > 1 ? mine < groups : i < pieces;
+        kv_floatx4 x = {};
+        if (works) {
+            const int first = groups > 1 ? mine : 0;
+            constexpr int kAhead = 8;
+            for (int c0 = first; c0 < nchunks; c0 += kAhead * groups) {
+                kv_floatx4 y[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const int c = c0 + k * groups < nchunks ? c0 + k * groups : c0;
+                    y[k] = __builtin_bit_cast(kv_floatx4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)((c * part_floats + row * D + d) * 4), 0, kAgent));
+                }
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                    if (c0 + k * groups < nchunks) x += y[k] * weight[(c0 + k * groups) * cap + row];
+            }
+        }
+        if (groups > 1) {
+            if (works) *reinterpret_cast<kv_floatx4 *>(meet + threadIdx.x * 4) = x;
+            __syncthreads();
+            if (mine == 0) {
+                for (int g = 1; g < groups; ++g) x += *reinterpret_cast<const kv_floatx4 *>(meet + (g * pieces + threadIdx.x) * 4);
+                store(row, d, x, inv_of[row]);
+            }
+        } else if (works) {
+            store(row, d, x, inv_of[row]);
+        }
     }
     // (every workgroup of the row tile has made its mark; two that both found all marks store the same results)
-    for (int i = threadIdx.x; i < nchunks; i += kWaves * 64) __hip_atomic_store(words + i, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int i = threadIdx.x; i < nchunks; i += WAVES * 64) __hip_atomic_store(words + i, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <int D>
+hipError_t launch_rows(const KvAttentionParams &p, hipStream_t stream) {
+    static LdsLimit limit;
+    constexpr int most = rows_lds_bytes(D, WAVES, 16, kKvMostChunks);
+    if (p.chunks > kKvMostChunks) return hipErrorInvalidValue;
+    if (most > 65536) {
+        const hipError_t e = limit.raise(reinterpret_cast<const void *>(kv_rows_kernel<D>), most);
+        if (e != hipSuccess) return e;
+    }
+    kv_rows_kernel<D><<<dim3(p.chunks, p.cache.heads, p.batch.sequences * p.row_tiles), WAVES * 64, rows_lds_bytes(D, WAVES, p.row_cap, p.chunks), stream>>>(p);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_kv_attention_rows(const KvAttentionParams &p, hipStream_t stream) {
-    const dim3 grid(p.chunks, p.cache.heads, p.batch.sequences * p.row_tiles);
     switch (p.cache.dim) {
-        case 64: kv_rows_kernel<64><<<grid, kWaves * 64, 0, stream>>>(p); break;
-        case 128: kv_rows_kernel<128><<<grid, kWaves * 64, 0, stream>>>(p); break;
-        case 256: kv_rows_kernel<256><<<grid, kWaves * 64, 0, stream>>>(p); break;
+        case 64: return launch_rows<64>(p, stream);
+        case 128: return launch_rows<128>(p, stream);
+        case 256: return launch_rows<256>(p, stream);
         default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
 
 }  // namespace svdq

@@ -88,8 +88,12 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void kv_tile_kernel(KvAttenti
         float x[C][8];
         uint32_t top = 0u;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {      // step c: channels 16 c + 8 h32 .. + 7
-            kv_rotated8(row, p.rope, pos, 16 * c + 8 * h32, x[c]);
+        for (int c = 0; c < C; c += 4) {      // step c: channels 16 c + 8 h32 .. + 7
+            kv_rotated<4>(row, p.rope, pos, [&](int i) { return 16 * (c + i) + 8 * h32; }, *reinterpret_cast<float(*)[4][8]>(&x[c]));
+            if (c + 4 < C) __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const uint32_t u = __float_as_uint(x[c][e]) & 0x7fffffffu;

@@ -772,34 +772,51 @@ constexpr int kKvTileRows = 128;
 constexpr unsigned long long kKvArrived = 0x4b56535644514152ull;      // as kActArrived: what a workgroup leaves in its arrival word
 // Rows of a sequence and key head up to which the kernel of few rows takes a launch (sixteen rows a workgroup; it reads the keys once per sixteen).
 constexpr int kKvFewRows = 32;
+constexpr int kKvMostChunks = 256;
 struct KvPlan {
     bool few;
-    int row_tiles, chunk_blocks, chunks;
-    size_t parts_off, ml_off, words_off, total;      // bytes of the workspace
+    int row_tiles, row_cap, chunk_blocks, chunks;
+    size_t parts_off, words_off, total;      // bytes of the workspace
 };
-inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len) {
+// Blocks of 32 keys of a chunk, for `blocks` of them in the longest sequence and `wgs` row tiles of all heads and sequences.  A workgroup costs 5 us
+// beside its blocks (0.15 us each while its CU is alone with it) and parts that meet 4.5 us more: one token on 1024 keys of eight heads takes 10.3 us whole
+// and 10.7 in pieces of 8 blocks, on 2048 keys 15.3 and 10.8.  So keys of at most 32 blocks stay whole; others are cut until there is a workgroup
+// for every CU, and for the sake of ragged batches into pieces of at most 256 blocks, at least 128 beyond one workgroup a CU: one sequence of 131071 keys 55.7 us in pieces of
+// 128, 58.6 of 64, 70.3 of 32; 64 sequences of up to 16384 keys 256 us in pieces of 256, 275 of 64, 374 of 16.
+inline int kv_chunk_blocks(long long wgs, int blocks) {
+    if (blocks <= 32 || wgs <= 0) return blocks;
+    const long long parts = wgs < 256 ? 256 / wgs : 1;
+    long long fill = (blocks + parts - 1) / parts, even = (blocks * wgs + 767) / 768;      // (three workgroups of a CU at a time)
+    if (fill < 8) fill = 8;
+    even = even < 128 ? 128 : even > 256 ? 256 : even;
+    long long c = fill < even ? fill : even;
+    const int least = (blocks + kKvMostChunks - 1) / kKvMostChunks;
+    return (int)(c < least ? least : c < blocks ? c : blocks);
+}
+// window: 0 or the keys that a row sees; it does not change the workspace
+inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len, int window) {
     KvPlan p{};
     const long long rows = (long long)max_new * group;
     p.few = rows <= kKvFewRows;
     p.row_tiles = p.few ? (int)((rows + 15) / 16) : 0;
+    p.row_cap = rows < 16 ? (int)rows : 16;
     p.chunks = 1;
-    const int blocks = (max_len + 31) / 32 > 0 ? (max_len + 31) / 32 : 1;
-    p.chunk_blocks = blocks;
-    if (p.few) {
-        const long long wgs = (long long)sequences * heads * (p.row_tiles > 0 ? p.row_tiles : 1);
-        long long want = (1024 + wgs - 1) / wgs;                             // about four workgroups per CU
-        if (want > (blocks + 7) / 8) want = (blocks + 7) / 8;                // two blocks a wavefront at least
-        p.chunk_blocks = (int)((blocks + want - 1) / want);
-        if (p.chunk_blocks > 64) p.chunk_blocks = 64;                        // long sequences of a ragged batch in pieces of 2048 tokens
-        p.chunks = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
-    }
     p.total = 256;
+    if (!p.few) return p;
+    const long long wgs = (long long)sequences * heads * p.row_tiles;
+    int blocks = max_len > 0 ? (max_len + 31) / 32 : 1;
+    p.chunk_blocks = kv_chunk_blocks(wgs, blocks);
+    p.chunks = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
     if (p.chunks > 1) {
         const size_t parts = (size_t)sequences * p.row_tiles * heads * p.chunks;
-        p.parts_off = 0;
-        p.ml_off = align256(parts * 16 * dim * 4);
-        p.words_off = p.ml_off + align256(parts * 16 * 2 * 4);
+        p.words_off = align256(parts * p.row_cap * (dim + 2) * 4);
         p.total = p.words_off + align256(parts * 8);
+    }
+    if (window > 0 && ((long long)window + max_new) / 32 + 2 < blocks) {      // no more chunks than the workspace has room for
+        blocks = (window + max_new) / 32 + 2;
+        const int c = kv_chunk_blocks(wgs, blocks), least = (blocks + p.chunks - 1) / p.chunks;
+        p.chunk_blocks = c > least ? c : least;
+        p.chunks = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
     }
     return p;
 }
