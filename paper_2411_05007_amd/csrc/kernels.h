@@ -244,10 +244,12 @@ struct KvAttentionParams {
     int q_heads, group;      // group = q_heads / cache.heads
     float scale;             // of the scores, times log2(e)
     int causal, window;      // window = 0: none
+    int tile_rows, parts;    // many-row kernel: rows of a workgroup (128 or 256), parts that the keys of a row tile are cut into
     int row_tiles;           // few-row kernel: tiles of 16 rows a sequence and head may need
     int row_cap;             // few-row kernel: rows that a tile can have
     int chunk_blocks, chunks;      // few-row kernel: the keys are cut into chunks of chunk_blocks blocks (the last takes the rest)
     float *partial;          // chunks > 1: fp32 [sequence][row tile][head][chunk]([row_cap][dim] sums, [row_cap][2] maximum and sum of weights)
+    float *part_ml;          // parts > 1: fp32 [part][row][2] maximum and sum of weights, rows as in out; partial [part][row][dim]
     unsigned long long *arrived;      // chunks > 1: [sequence][row tile][head][chunk]
 };
 hipError_t launch_kv_attention_rows(const KvAttentionParams &p, hipStream_t stream);      // few rows (kv_rows_kernel.hip)

@@ -66,10 +66,12 @@ template <int D>
 __global__ __launch_bounds__(128) void kv_append_kernel(KvAppendParams p, int heads_per_wg) {
     __shared__ uint32_t bad_of[2][2];      // vectors that are not finite: [head's parity][keys, values]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int local, t0, n;
-    const int b = kv_item_sequence<2, kKvBlock>(p.batch.cu, p.batch.sequences, p.batch.total, 1, blockIdx.x, local);
-    kv_range(p.batch.cu, b, p.batch.total, t0, n);
-    const int len = kv_length(p.cache, p.batch, b), before = len - n;      // (before < 0: the first -before tokens have no place in the sequence)
+    const KvItem item = kv_item(p.batch, blockIdx.x, [&](int n, int value) {
+        const int len = kv_length(p.cache, p.batch, value), first = len > n ? len - n : 0;
+        return n > 0 ? ((len + 31) >> 5) - (first >> 5) : 0;
+    });
+    const int b = item.sequence, local = item.local, t0 = item.first, n = item.count;
+    const int len = kv_length(p.cache, p.batch, item.value), before = len - n;      // (before < 0: the first -before tokens have no place in the sequence)
     const int first_pos = before < 0 ? 0 : before;
     const int blk = (first_pos >> 5) + local;
     if (local < 0 || blk * kKvBlock >= len || n == 0) return;
@@ -237,11 +239,11 @@ __device__ __forceinline__ uint32_t bf16_pair(uint32_t w, float scale, bool high
 template <int D>
 __global__ __launch_bounds__(128) void kv_gather_kernel(KvGatherParams p) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int local, r0, n;
-    const int b = kv_item_sequence<2, kKvBlock>(p.batch.cu, p.batch.sequences, p.batch.total, 1, blockIdx.x, local);
-    kv_range(p.batch.cu, b, p.batch.total, r0, n);
-    int start = p.batch.kv_len[b];
-    start = __builtin_amdgcn_readfirstlane(start < 0 ? 0 : start);
+    const KvItem item = kv_item(p.batch, blockIdx.x, [](int n, int value) {
+        const long long start = value < 0 ? 0 : value;
+        return n > 0 ? (int)((start + n + 31) / 32 - start / 32) : 0;
+    });
+    const int b = item.sequence, local = item.local, r0 = item.first, n = item.count, start = item.value < 0 ? 0 : item.value;
     const int blk = (start >> 5) + local;
     const long long end = (long long)start + n;
     if (local < 0 || n == 0 || (long long)blk * kKvBlock >= end) return;

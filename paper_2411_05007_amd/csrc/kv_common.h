@@ -34,45 +34,50 @@ typedef uint32_t kv_u32x2 __attribute__((ext_vector_type(2)));
 __host__ __device__ constexpr int kv_slot_token(int g) { return 16 * (g >> 1) + 4 * (g & 1); }
 
 // ---- work items of a ragged batch -----------------------------------------------------------------------------------------
-// Sequence b owns the items from floor(cu[b] / UNIT) + EXTRA b on: room for ceil(n / UNIT) items (EXTRA = 1), or for the aligned units that n
-// tokens from any position on touch (EXTRA = 2), for any lengths, so a grid of floor(T / UNIT) + EXTRA B items is enough without the lengths
-// on the host.  All lanes look at once: 64 sequences a round.  cu is taken as far as it ascends within 0 .. T.
-template <int EXTRA, int UNIT>
-__device__ __forceinline__ int kv_item_sequence(const int32_t *cu, int sequences, int total, int mul, int item, int &local) {
+// The sequences' items lie behind each other: a workgroup finds its own by a scan over how many each sequence has, 64 sequences a round, from lengths
+// that the host need not know; a grid of more items than there are is empty at its end only.  (With room for every sequence's remainder behind its own items, every other
+// workgroup of equal short sequences was empty, the dispatcher put the others on half of the CUs, and 32 sequences of 128 rows on 4128 keys took 259 us instead of 162.)
+// cu is taken within 0 .. T, as far as it ascends.
+struct KvItem { int sequence, local, first, count, value; };      // local: which item of the sequence, -1: none; its tokens; kv_len as it stands
+__device__ __forceinline__ int kv_within(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+template <typename Units>
+__device__ __forceinline__ KvItem kv_item(const KvBatch &t, int item, Units units) {      // units(count, value): items of a sequence
     const int lane = threadIdx.x & 63;
-    int count = 0;
-    for (int b0 = 0; b0 < sequences; b0 += 64) {
-        const int b = b0 + lane;
-        bool owns = false;
-        if (b < sequences) {
-            int at = cu[b];
-            at = at < 0 ? 0 : at > total ? total : at;
-            owns = (int)((long long)at * mul / UNIT) + EXTRA * b <= item;
+    KvItem got{0, -1, 0, 0, 0};
+    for (int b0 = 0; b0 < t.sequences; b0 += 64) {
+        const int b = b0 + lane < t.sequences ? b0 + lane : t.sequences - 1;
+        const int first = kv_within(t.cu[b], 0, t.total), count = kv_within(t.cu[b + 1], first, t.total) - first, value = t.kv_len[b];
+        const int mine = b0 + lane < t.sequences ? units(count, value) : 0;
+        int upto = mine;
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) {
+            const int y = __shfl_up(upto, s);
+            upto += lane >= s ? y : 0;
         }
-        const unsigned long long set = __builtin_amdgcn_ballot_w64(owns);
-        count += __builtin_popcountll(set);
-        if (set != ~0ull) break;
+        const unsigned long long past = __builtin_amdgcn_ballot_w64(upto > item);
+        if (past != 0ull) {
+            const int at = __builtin_ctzll(past);
+            got.sequence = b0 + at;
+            got.local = item - __builtin_amdgcn_readlane(upto - mine, at);
+            got.first = __builtin_amdgcn_readlane(first, at);
+            got.count = __builtin_amdgcn_readlane(count, at);
+            got.value = __builtin_amdgcn_readlane(value, at);
+            break;
+        }
+        item -= __builtin_amdgcn_readlane(upto, 63);
     }
-    const int b = count > 0 ? count - 1 : 0;
-    int at = cu[b];
-    at = at < 0 ? 0 : at > total ? total : at;
-    local = item - ((int)((long long)at * mul / UNIT) + EXTRA * b);
-    return __builtin_amdgcn_readfirstlane(b);
+    return got;
 }
 // sequence b's tokens within 0 .. total
 __device__ __forceinline__ void kv_range(const int32_t *cu, int b, int total, int &first, int &count) {
-    int lo = cu[b], hi = cu[b + 1];
-    lo = lo < 0 ? 0 : lo > total ? total : lo;
-    hi = hi < lo ? lo : hi > total ? total : hi;
+    const int lo = kv_within(cu[b], 0, total), hi = kv_within(cu[b + 1], lo, total);
     first = __builtin_amdgcn_readfirstlane(lo);
     count = __builtin_amdgcn_readfirstlane(hi - lo);
 }
-// tokens of sequence b that the cache can hold
-__device__ __forceinline__ int kv_length(const KvCache &c, const KvBatch &t, int b) {
-    int len = t.kv_len[b];
+// tokens of a sequence that the cache can hold
+__device__ __forceinline__ int kv_length(const KvCache &c, const KvBatch &t, int len) {
     const long long most = (long long)t.table_width << c.page_shift;
-    len = len < 0 ? 0 : (long long)len > most ? (int)most : len;
-    return __builtin_amdgcn_readfirstlane(len);
+    return len < 0 ? 0 : (long long)len > most ? (int)most : len;
 }
 // (page, head, block within the page) of block `blk` of sequence b as an index of the scale arrays, -1 where the table names no page of the cache
 __device__ __forceinline__ long long kv_unit(const KvCache &c, const int32_t *table, int width, int b, int head, int blk) {

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     const int head = blockIdx.y, b = blockIdx.z / p.row_tiles, tile = blockIdx.z % p.row_tiles;
     int t0, n;
     kv_range(p.batch.cu, b, p.batch.total, t0, n);
-    const int len = kv_length(p.cache, p.batch, b), rows = n * p.group;
+    const int len = __builtin_amdgcn_readfirstlane(kv_length(p.cache, p.batch, p.batch.kv_len[b])), rows = n * p.group;
     if (tile * 16 >= rows) return;
     // the lane's row and the keys [seen_lo, seen_hi) that it sees
     const int r = tile * 16 + l16 < rows ? tile * 16 + l16 : rows - 1;

@@ -768,17 +768,15 @@ inline Workspace workspace_layout(int M, int K, int N, int rank, int ksplit_over
 }
 
 // ---- attention over the paged 8-bit cache: which kernel, and how the keys are cut --------------------------------------------------------
-constexpr int kKvTileRows = 128;
 constexpr unsigned long long kKvArrived = 0x4b56535644514152ull;      // as kActArrived: what a workgroup leaves in its arrival word
-// Rows of a sequence and key head up to which the kernel of few rows takes a launch (sixteen rows a workgroup; it reads the keys once per sixteen).
-constexpr int kKvFewRows = 32;
 constexpr int kKvMostChunks = 256;
 struct KvPlan {
-    bool few;
-    int row_tiles, row_cap, chunk_blocks, chunks;
-    size_t parts_off, words_off, total;      // bytes of the workspace
+    bool few;                                          // the kernel of sixteen rows a workgroup (kv_rows_kernel.hip), or of 128 or 256 (kv_tile_kernel.hip)
+    int row_tiles, row_cap, chunk_blocks, chunks;      // few
+    int tile_rows, parts;                              // many
+    size_t words_off, ml_off, total;                   // bytes of the workspace (partial sums lie at its start)
 };
-// Blocks of 32 keys of a chunk, for `blocks` of them in the longest sequence and `wgs` row tiles of all heads and sequences.  A workgroup costs 5 us
+// Few: blocks of 32 keys of a chunk, for `blocks` of them in the longest sequence and `wgs` row tiles of all heads and sequences.  A workgroup costs 5 us
 // beside its blocks (0.15 us each while its CU is alone with it) and parts that meet 4.5 us more: one token on 1024 keys of eight heads takes 10.3 us whole
 // and 10.7 in pieces of 8 blocks, on 2048 keys 15.3 and 10.8.  So keys of at most 32 blocks stay whole; others are cut until there is a workgroup
 // for every CU, and for the sake of ragged batches into pieces of at most 256 blocks, at least 128 beyond one workgroup a CU: one sequence of 131071 keys 55.7 us in pieces of
@@ -793,16 +791,52 @@ inline int kv_chunk_blocks(long long wgs, int blocks) {
     const int least = (blocks + kKvMostChunks - 1) / kKvMostChunks;
     return (int)(c < least ? least : c < blocks ? c : blocks);
 }
-// window: 0 or the keys that a row sees; it does not change the workspace
-inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len, int window) {
+// Many: parts of the keys of a row tile, each at least eight tiles of 64 keys, so that the parts of all row tiles are one round of the CUs (two workgroups of
+// 128 rows on each): 256 rows on 16000 keys of one head 343 us whole, 101 in 4 parts, 49 in 16, 60 in 32; 1200 rows of four sequences on
+// 8000 keys of two heads 182, 83 in 4, 81 in 8, 91 in 16.  `wgs`: row tiles of all heads and sequences; `keys`: that a row tile sees.
+inline int kv_parts(long long wgs, long long slots, long long keys) {
+    long long n = wgs > 0 ? slots / wgs : 1;
+    n = n > keys / 512 ? keys / 512 : n;
+    return n < 1 ? 1 : n > 16 ? 16 : (int)n;
+}
+// The kernel by what each is estimated to cost, in ns.  Few: 10 us, and 0.75 ns for a row tile and block of all CUs (head size 128).  Many: 15 us, 12 more where parts meet, and
+// 2.2 us for each 64 keys of a round of workgroups.  Measured, us, few | many: 64 sequences of 64 rows (eight key heads) on 4000 keys 169 | 150, of 128
+// rows 298 | 155, eight sequences of 64 rows 29 | 41, of 256 rows 75 | 57, one of 256 rows on 16000 keys 58 | 74, on 500 12 | 22; four of 128 rows (24
+// heads) on 1128 keys 25 | 34; 16 of 256 rows (16 heads of 64) on 512 keys 36 | 24.
+inline bool kv_few_rows(int sequences, int heads, int dim, long long rows, int max_len) {
+    const long long tiles = (rows + 15) / 16, blocks = (max_len + 31) / 32;
+    if (rows <= 16) return true;
+    if (sequences * tiles > 65535) return false;      // (the grid of that kernel)
+    const long long slots = dim == 256 ? 256 : 512, wgs = sequences * ((rows + 127) / 128) * heads;
+    const int parts = kv_parts(wgs, slots, max_len);
+    const double few = 10000.0 + 0.75 * (double)(sequences * tiles * heads) * (double)blocks * dim / 128.0;
+    const double rounds = (double)(wgs * parts) / (double)slots;
+    const double many = 15000.0 + (parts > 1 ? 12000.0 : 0.0) + (rounds > 1.0 ? rounds : 1.0) * 2200.0 * (double)max_len / 64.0 / parts * dim / 128.0;
+    return few <= many;
+}
+// window: 0 or the keys that a row sees; it does not change the kernel, and asks for no more workspace than none.  even: all sequences have max_new tokens.
+inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len, int window, bool even) {
     KvPlan p{};
     const long long rows = (long long)max_new * group;
-    p.few = rows <= kKvFewRows;
-    p.row_tiles = p.few ? (int)((rows + 15) / 16) : 0;
-    p.row_cap = rows < 16 ? (int)rows : 16;
-    p.chunks = 1;
+    p.few = kv_few_rows(sequences, heads, dim, rows, max_len);
+    p.chunks = p.parts = 1;
     p.total = 256;
-    if (!p.few) return p;
+    if (!p.few) {
+        // 256 rows, one workgroup on a CU, stage a tile of keys for twice the rows: 8192 tokens x 4 heads on 16384 keys 1539 us (128 rows: 1618), joint attention of 4608
+        // tokens 281 (300); but what is masked or left over is larger: ragged chunks 357 (355), 7409 rows x 2 in a window 498 (469).
+        const long long large = (long long)sequences * ((rows + 255) / 256) * heads, small = (long long)sequences * ((rows + 127) / 128) * heads;
+        p.tile_rows = dim == 128 && even && window == 0 && max_len >= 4096 && large >= 256 ? 256 : 128;
+        const long long keys = window > 0 && (long long)window + 128 / group < max_len ? (long long)window + 128 / group : max_len;
+        p.parts = p.tile_rows == 256 ? 1 : kv_parts(small, dim == 256 ? 256 : 512, keys);
+        if (p.parts > 1) {
+            const size_t all = (size_t)p.parts * sequences * max_new * heads * group;
+            p.ml_off = align256(all * dim * 4);
+            p.total = p.ml_off + align256(all * 8);
+        }
+        return p;
+    }
+    p.row_tiles = (int)((rows + 15) / 16);
+    p.row_cap = rows < 16 ? (int)rows : 16;
     const long long wgs = (long long)sequences * heads * p.row_tiles;
     int blocks = max_len > 0 ? (max_len + 31) / 32 : 1;
     p.chunk_blocks = kv_chunk_blocks(wgs, blocks);
