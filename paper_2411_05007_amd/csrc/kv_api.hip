@@ -9,6 +9,7 @@ namespace {
 
 constexpr int kMaxTokens = 1 << 30;      // of a sequence: positions and key indices are 32-bit with room to add a tile
 constexpr int kMaxGridY = 65535;
+constexpr int64_t kMostStride = 1 << 25;
 
 int check_shape(const svdq_kv_shape &s) {
     if (s.kv_heads <= 0 || s.head_dim <= 0 || s.page_tokens <= 0) return SVDQ_EINVAL;
@@ -38,7 +39,8 @@ int check_rope(const svdq_kv_rope *r, int dim) {
 }
 int check_rows(const svdq_kv_rows *r) {
     if (!r || !r->data || ((uintptr_t)r->data & 15)) return SVDQ_EINVAL;
-    return r->token_stride % 8 != 0 || r->head_stride % 8 != 0 ? SVDQ_EINVAL : SVDQ_OK;
+    if (r->token_stride % 8 != 0 || r->head_stride % 8 != 0 || r->token_stride < 0 || r->head_stride < 0) return SVDQ_EINVAL;
+    return r->token_stride > kMostStride ? SVDQ_EUNSUPPORTED : SVDQ_OK;      // (the rows of a block are addressed with 32 bits from its first)
 }
 svdq::KvCache cache_of(const svdq_kv_cache_dev *c) {
     svdq::KvCache k{};
