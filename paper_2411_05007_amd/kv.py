@@ -19,6 +19,9 @@ import torch
 from . import svdq as S
 
 
+_current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else lambda i: torch.cuda.current_stream(i).cuda_stream
+
+
 def _device_int32(t, name: str) -> None:
     assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous(), f"{name}: contiguous int32 on the GPU"
 
@@ -68,6 +71,7 @@ class KVRows:
         B = first_token.shape[0]
         assert cu_rows.shape == (B + 1,) and block_table.dim() == 2 and block_table.shape[0] == B
         self.first_token, self.cu_rows, self.block_table, self.sequences, self.rows = first_token, cu_rows, block_table, B, int(rows)
+        self.pointers, self.width = (first_token.data_ptr(), cu_rows.data_ptr(), block_table.data_ptr()), block_table.shape[1]
 
 
 class KVCache:
@@ -102,12 +106,14 @@ class KVCache:
         self.cdesc = S.KVCacheDev(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), pages, self.shape)
 
     def _rows(self, t, heads: Optional[int], tokens: int, name: str):
-        assert t.dtype == torch.bfloat16 and t.is_cuda and t.dim() == 3 and t.stride(2) == 1, f"{name}: bf16 [tokens, heads, head_dim] on the GPU, channels next to each other"
-        assert t.shape[0] == tokens and t.shape[2] == self.head_dim and (heads is None or t.shape[1] == heads), f"{name}: shape {tuple(t.shape)}"
-        return S.KVRowsDev(t.data_ptr(), t.stride(0), t.stride(1))
+        shape = t.shape
+        assert len(shape) == 3 and shape[0] == tokens and shape[2] == self.head_dim and (heads is None or shape[1] == heads), f"{name}: shape {tuple(shape)}"
+        token, head, channel = t.stride()
+        assert t.dtype is torch.bfloat16 and t.is_cuda and channel == 1, f"{name}: bf16 [tokens, heads, head_dim] on the GPU, channels next to each other"
+        return S.KVRowsDev(t.data_ptr(), token, head)
 
     def _stream(self, stream):
-        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+        return _current_stream(self.device.index) if stream is None else stream.cuda_stream
 
     def append(self, k, v, batch: KVBatch, rope: Optional[Rope] = None, stream=None) -> None:
         """k, v: bf16 [new_tokens, kv_heads, head_dim] (any token and head stride that keeps 16-byte alignment)."""
@@ -128,7 +134,7 @@ class KVCache:
         if out is None:
             out = torch.empty((batch.new_tokens, heads, self.head_dim), dtype=torch.bfloat16, device=q.device)
         else:
-            assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == q.shape
+            assert out.dtype is torch.bfloat16 and out.is_cuda and out.is_contiguous() and out.shape == q.shape
         if workspace is None:
             workspace = self.attention_workspace(batch, heads)
         S._check(S.lib().svdq_kv_attention(self.cdesc, batch.cdesc, None if rope is None else rope.cdesc, qd, heads,
@@ -142,7 +148,7 @@ class KVCache:
         if out is None:
             out = [torch.empty(shape, dtype=torch.bfloat16, device=self.device) for _ in range(2)]
         for t in out:
-            assert t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == shape
-        S._check(S.lib().svdq_kv_gather(self.cdesc, rows.first_token.data_ptr(), rows.cu_rows.data_ptr(), rows.block_table.data_ptr(), rows.sequences,
-                                        rows.block_table.shape[1], rows.rows, out[0].data_ptr(), out[1].data_ptr(), self._stream(stream)), "svdq_kv_gather")
+            assert t.dtype is torch.bfloat16 and t.is_cuda and t.is_contiguous() and t.shape == shape
+        S._check(S.lib().svdq_kv_gather(self.cdesc, *rows.pointers, rows.sequences, rows.width, rows.rows, out[0].data_ptr(), out[1].data_ptr(), self._stream(stream)),
+                 "svdq_kv_gather")
         return out
