@@ -444,7 +444,8 @@ int svdq_kv_append(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, c
  * so that none is lost to its range), codes times scales are exact.  A row that sees no key is zero.
  *   out: device bf16 [new_tokens][q_heads][head_dim], 16-byte aligned
  *   workspace: device, 256-byte aligned, >= svdq_kv_attention_workspace_bytes(); needs no initial contents.  Two calls that share one must be ordered on one stream.
- * One kernel.
+ * One kernel; a second one adds the parts where the keys of many rows are cut.  The kernel and the cut follow from sequences, heads, max_new, max_len and
+ * window alone, so the same call gives the same bits.
  */
 size_t svdq_kv_attention_workspace_bytes(const svdq_kv_shape *shape, int q_heads, int sequences, int max_new, int max_len);
 int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope, const svdq_kv_rows *q,
