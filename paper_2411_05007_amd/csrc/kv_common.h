@@ -40,6 +40,13 @@ __host__ __device__ constexpr int kv_slot_token(int g) { return 16 * (g >> 1) + 
 // cu is taken within 0 .. T, as far as it ascends.
 struct KvItem { int sequence, local, first, count, value; };      // local: which item of the sequence, -1: none; its tokens; kv_len as it stands
 __device__ __forceinline__ int kv_within(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+// sum over the lanes up to this one
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ int kv_add_dpp(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CONTROL, ROWS, 0xf, true); }
+__device__ __forceinline__ int kv_sum_upto(int x) {
+    x = kv_add_dpp<0x118, 0xf>(kv_add_dpp<0x114, 0xf>(kv_add_dpp<0x112, 0xf>(kv_add_dpp<0x111, 0xf>(x))));      // within sixteen lanes: from 1, 2, 4, 8 lanes below
+    return kv_add_dpp<0x143, 0xc>(kv_add_dpp<0x142, 0xa>(x));      // the second and fourth sixteen take the last lane before them, then the upper half lane 31
+}
 template <typename Units>
 __device__ __forceinline__ KvItem kv_item(const KvBatch &t, int item, Units units) {      // units(count, value): items of a sequence
     const int lane = threadIdx.x & 63;
@@ -48,12 +55,7 @@ __device__ __forceinline__ KvItem kv_item(const KvBatch &t, int item, Units unit
         const int b = b0 + lane < t.sequences ? b0 + lane : t.sequences - 1;
         const int first = kv_within(t.cu[b], 0, t.total), count = kv_within(t.cu[b + 1], first, t.total) - first, value = t.kv_len[b];
         const int mine = b0 + lane < t.sequences ? units(count, value) : 0;
-        int upto = mine;
-#pragma unroll
-        for (int s = 1; s < 64; s *= 2) {
-            const int y = __shfl_up(upto, s);
-            upto += lane >= s ? y : 0;
-        }
+        const int upto = kv_sum_upto(mine);
         const unsigned long long past = __builtin_amdgcn_ballot_w64(upto > item);
         if (past != 0ull) {
             const int at = __builtin_ctzll(past);
@@ -216,6 +218,19 @@ __device__ __forceinline__ void kv_swap16(float x, float &a, float &b) {
 }
 __device__ __forceinline__ float kv_max32(float x) { float a, b; kv_swap32(x, a, b); return fmaxf(a, b); }
 __device__ __forceinline__ float kv_max16(float x) { float a, b; kv_swap16(x, a, b); return fmaxf(a, b); }
+// over U = 4, 8 or 16 neighbouring lanes, NaN if one is NaN
+template <int CONTROL>
+__device__ __forceinline__ float kv_max_dpp(float x) {
+    const int y = __builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CONTROL, 0xf, 0xf, false);
+    return __builtin_elementwise_maximum(x, __uint_as_float((uint32_t)y));
+}
+template <int U>
+__device__ __forceinline__ float kv_max_lanes(float x) {
+    x = kv_max_dpp<0x4e>(kv_max_dpp<0xb1>(x));      // quads: lanes 1, 0, 3, 2, then 2, 3, 0, 1
+    if (U >= 8) x = kv_max_dpp<0x141>(x);           // eight lanes backwards
+    if (U >= 16) x = kv_max_dpp<0x140>(x);          // sixteen
+    return x;
+}
 __device__ __forceinline__ float kv_sum32(float x) { float a, b; kv_swap32(x, a, b); return a + b; }
 __device__ __forceinline__ float kv_sum16(float x) { float a, b; kv_swap16(x, a, b); return a + b; }
 

@@ -58,6 +58,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     const int wg_lo = lo_of(pos_of(row0)), wg_hi = hi_of(pos_of(row0 + kRows - 1));
     const int w_first = pos_of(row0 + wave * 32), w_last = pos_of(row0 + wave * 32 + 31);
     const int all_lo = lo_of(w_last), all_hi = hi_of(w_first);
+    const bool idle = row0 + wave * 32 >= rows;      // no row is left for the wavefront: it brings codes to LDS, and leaves its SIMD to the others
     // tiles of keys, and this part's share of them
     const int key_a = wg_lo / kTileKeys * kTileKeys, tiles_a = wg_hi > key_a ? (wg_hi - key_a + kTileKeys - 1) / kTileKeys : 0;
     const int tile0 = (int)((long long)tiles_a * part / p.parts), tiles_k = (int)((long long)tiles_a * (part + 1) / p.parts) - tile0;
@@ -140,13 +141,15 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     // (the two runs of eight that the rotation pairs), neighbouring lanes with neighbouring channels; each wavefront turns its rows and lays them down in its own part of
     // LDS as operands. ----
     kv_f16x8 qf[C];
-    float to_t;      // score -> exponent of 2, but for the block's scale; not negative: a negative scale turns the queries' sign
+    float to_t = 0.f;      // score -> exponent of 2, but for the block's scale; not negative: a negative scale turns the queries' sign
+    constexpr int U = D / 16, PER = U < 8 ? U / 2 : 4;      // units of a row, of a lane at a time
+    constexpr int kChunk = 33 * 16;         // bytes of a run of eight channels of 32 rows in LDS
+    unsigned char *my_queries = lds + wave * (2 * U * kChunk + 128);
+    float *factors = reinterpret_cast<float *>(my_queries + 2 * U * kChunk);
     look_up_pages(0);
-    {
-        constexpr int U = D / 16, PER = U < 8 ? U / 2 : 4;      // units of a row, of a lane at a time
-        constexpr int kChunk = 33 * 16;         // bytes of a run of eight channels of 32 rows in LDS
-        unsigned char *mine = lds + wave * (2 * U * kChunk + 128);
-        float *factors = reinterpret_cast<float *>(mine + 2 * U * kChunk);
+    if (idle) {
+        look_up_bytes(0);
+    } else {
         const int half = p.rope.dims / 2;
         for (int i0 = 0; i0 < U / 2; i0 += PER) {
             uint4 own[PER][2];
@@ -181,30 +184,26 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
                 const float cc[8] = {c[i][0].x, c[i][0].y, c[i][0].z, c[i][0].w, c[i][1].x, c[i][1].y, c[i][1].z, c[i][1].w};
                 const float ss[8] = {s[i][0].x, s[i][0].y, s[i][0].z, s[i][0].w, s[i][1].x, s[i][1].y, s[i][1].z, s[i][1].w};
                 if (turn) {
+                    if (!p.rope.interleaved) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (halves) {
+                        for (int e = 0; e < 8; ++e) {
                             const float a = x[0][e], y = x[1][e];
                             x[0][e] = kv_turn_a(a, y, cc[e], ss[e]);
                             x[1][e] = kv_turn_b(a, y, cc[e], ss[e]);
-                        } else {
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
                             const float a = x[e / 4][2 * (e % 4)], y = x[e / 4][2 * (e % 4) + 1];
                             x[e / 4][2 * (e % 4)] = kv_turn_a(a, y, cc[e], ss[e]);
                             x[e / 4][2 * (e % 4) + 1] = kv_turn_b(a, y, cc[e], ss[e]);
                         }
                     }
                 }
-                uint32_t top = 0u;
+                float most = 0.f;      // (NaN if one is NaN)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const uint32_t v = __float_as_uint(x[e / 8][e % 8]) & 0x7fffffffu;
-                    top = top > v ? top : v;
-                }
-#pragma unroll
-                for (int m = 1; m < U; m *= 2) {      // (the row's units are neighbouring lanes)
-                    const uint32_t v = (uint32_t)__shfl_xor((int)top, m);
-                    top = top > v ? top : v;
-                }
+                for (int e = 0; e < 8; ++e) most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(most, __builtin_fabsf(x[0][e])), __builtin_fabsf(x[1][e]));
+                const uint32_t top = __float_as_uint(kv_max_lanes<U>(most)) & 0x7fffffffu;      // (the row's units are neighbouring lanes)
                 const int e = (int)((top >= 0x7f800000u ? 0x7f800000u : top) >> 23) - 127;      // largest in [2^e, 2^(e + 1))
                 const int up = e < -100 ? 114 : e > 127 ? 0 : 14 - e;                           // (not finite: as it is, the row becomes NaN)
                 const float f = p.scale < 0.f ? -kv_pow2(up) : kv_pow2(up);
@@ -214,15 +213,11 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
 #pragma unroll
                     for (int k = 0; k < 8; ++k) w[k] = (_Float16)(x[j][k] * f);
                     const int chunk = halves ? pr + j * (half / 8) : 2 * pr + j;
-                    *reinterpret_cast<kv_f16x8 *>(mine + chunk * kChunk + row * 16) = w;
+                    *reinterpret_cast<kv_f16x8 *>(my_queries + chunk * kChunk + row * 16) = w;
                 }
                 if (pr == 0) factors[row] = __builtin_fabsf(p.scale) * kv_pow2(-up);
             }
         }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int c = 0; c < C; ++c) qf[c] = *reinterpret_cast<const kv_f16x8 *>(mine + (2 * c + h32) * kChunk + l32 * 16);      // step c: channels 16 c + 8 h32 .. + 7
-        to_t = factors[l32];
     }
     uint4 kw[2][N], vw[2][N];      // codes on their way: of keys and values of even and odd tiles
     next_window();
@@ -232,6 +227,12 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         request(vw[0], p.cache.v, f0);
         request(kw[1], p.cache.k, f1);
         request(vw[1], p.cache.v, f1);
+    }
+    if (!idle) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int c = 0; c < C; ++c) qf[c] = *reinterpret_cast<const kv_f16x8 *>(my_queries + (2 * c + h32) * kChunk + l32 * 16);      // step c: channels 16 c + 8 h32 .. + 7
+        to_t = factors[l32];
     }
     kv_lds_barrier();      // (the tiles go where the queries lie)
 
@@ -304,9 +305,18 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
 
     // Tile t + 1's scores are made beside tile t's weights; in LDS the keys are a tile ahead of the values:
     //   step t: S(t + 1) from keys t + 1, P(t) from S(t), O += P(t) V(t); keys t + 2 and values t + 1 go to LDS, keys t + 4 and values t + 3 are requested
+    auto advance = [&](int far) {      // facts of the next step: tile `far` comes in
+        if ((far & 7) == 0) {
+            if ((far & 31) == 8) look_up_pages(far + 24);
+            else if ((far & 31) == 16) look_up_bytes(far + 16);
+            else if ((far & 31) == 0) next_window();
+        }
+        f1 = f2;
+        f2 = f3;
+        f3 = f4;
+        f4 = facts_of(far);
+    };
     if (tiles_k > 0) {
-        Scores even, odd;
-        float top[2];
         ref = refer(f0);
         clear_unnamed(vw[0], f0);
 #pragma unroll
@@ -320,6 +330,29 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         for (int i = 0; i < N; ++i) keys_to_lds(kw[1], kt(1), i);
         request(kw[1], p.cache.k, f3);
         kv_lds_barrier();
+    }
+    if (tiles_k > 0 && idle) {      // a wavefront's part of the steps but for its products
+        kv_lds_barrier();
+        auto carry = [&](uint4 (&kn)[N], uint4 (&vn)[N], int t) {
+            ref = refer(f1) > ref ? refer(f1) : ref;
+            clear_unnamed(vn, f1);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                values_to_lds(vn, vt(t + 1), f1, t + 1, ref, i, std::true_type{});
+                keys_to_lds(kn, kt(t), i);
+            }
+            request(vn, p.cache.v, f3);
+            request(kn, p.cache.k, f4);
+            kv_lds_barrier();
+            advance(t + 5);
+        };
+        for (int t = 0; t + 1 < tiles_k; t += 2) {
+            carry(kw[0], vw[1], t);
+            if (t + 2 < tiles_k) carry(kw[1], vw[0], t + 1);
+        }
+    } else if (tiles_k > 0) {
+        Scores even, odd;
+        float top[2];
         even[0] = even[1] = kv_floatx16{};
 #pragma unroll
         for (int k = 0; k < 2 * C; ++k) even[k & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_operand(kt(0), k / 2, k & 1), qf[k / 2], even[k & 1], 0, 0, 0);
@@ -384,16 +417,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
             grow(held);
             look_at(next, top, f1, t + 1);
             kv_lds_barrier();
-            const int far = t + 5;
-            if ((far & 7) == 0) {
-                if ((far & 31) == 8) look_up_pages(far + 24);
-                else if ((far & 31) == 16) look_up_bytes(far + 16);
-                else if ((far & 31) == 0) next_window();
-            }
-            f1 = f2;
-            f2 = f3;
-            f3 = f4;
-            f4 = facts_of(far);
+            advance(t + 5);
         };
         int t = 0;
         for (; t + 4 <= tiles_k; t += 2) {      // (the last tile's values may be partial: step tiles_k - 2)
@@ -431,20 +455,21 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         if (tiles_k == 0) return;
     }
     kv_lds_barrier();      // (the last tiles are read)
+    if (idle) return;
     constexpr int kOut = 64, kOutRow = kOut * 4 + 16;      // channels of a round and bytes of a row, fp32
-    unsigned char *mine = lds + wave * 32 * kOutRow;
+    unsigned char *my_rows = lds + wave * 32 * kOutRow;
 #pragma unroll
     for (int a0 = 0; a0 < A; a0 += 2) {
 #pragma unroll
         for (int a = a0; a < a0 + 2; ++a)
 #pragma unroll
             for (int v = 0; v < 16; v += 4)
-                *reinterpret_cast<float4 *>(mine + l32 * kOutRow + (32 * (a - a0) + 2 * v + 4 * h32) * 4) = make_float4(o[a][v] * f, o[a][v + 1] * f, o[a][v + 2] * f, o[a][v + 3] * f);
+                *reinterpret_cast<float4 *>(my_rows + l32 * kOutRow + (32 * (a - a0) + 2 * v + 4 * h32) * 4) = make_float4(o[a][v] * f, o[a][v + 1] * f, o[a][v + 2] * f, o[a][v + 3] * f);
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {      // eight channels a lane, eight rows a time
             const int row = 8 * i + lane / 8, d = lane % 8 * 8, r = row0 + wave * 32 + row;
-            const float4 x = *reinterpret_cast<const float4 *>(mine + row * kOutRow + d * 4), y = *reinterpret_cast<const float4 *>(mine + row * kOutRow + d * 4 + 16);
+            const float4 x = *reinterpret_cast<const float4 *>(my_rows + row * kOutRow + d * 4), y = *reinterpret_cast<const float4 *>(my_rows + row * kOutRow + d * 4 + 16);
             if (r >= rows) continue;
             if (parts) {
                 float *dst = p.partial + (part * out_rows + out_row(r)) * D + 32 * a0 + d;
