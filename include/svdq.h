@@ -418,7 +418,7 @@ typedef struct {
     const int32_t *cu_new, *kv_len, *block_table; /* device: [sequences + 1], [sequences], [sequences][table_width] */
     int sequences, table_width;
     int new_tokens; /* of all sequences */
-    int max_new;    /* no sequence has more new tokens (attention: chooses the kernel; tokens past it are refused a row) */
+    int max_new;    /* no sequence has more new tokens (attention: chooses the kernels; tokens past it may be refused a row) */
     int max_len;    /* no kv_len is larger (attention: how the keys are cut; larger ones are right, but slower) */
 } svdq_kv_batch;
 typedef struct {
@@ -444,8 +444,9 @@ int svdq_kv_append(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, c
  * so that none is lost to its range), codes times scales are exact.  A row that sees no key is zero.
  *   out: device bf16 [new_tokens][q_heads][head_dim], 16-byte aligned
  *   workspace: device, 256-byte aligned, >= svdq_kv_attention_workspace_bytes(); needs no initial contents.  Two calls that share one must be ordered on one stream.
- * One kernel; a second one adds the parts where the keys of many rows are cut.  The kernel and the cut follow from sequences, heads, max_new, max_len and
- * window alone, so the same call gives the same bits.
+ *   Its size: up to 34 MB for the parts of chunks, and for single tokens the fp32 sums of up to 16 rows for each sequence, key head and 4096 to 8192 keys.
+ * One kernel, or one for the sequences with chunks and one for those of single tokens; a further one adds the parts where the keys of many rows are cut.  What is
+ * launched, and the cut, follow from the sizes in batch and shape and from window, so the same call gives the same bits.
  */
 size_t svdq_kv_attention_workspace_bytes(const svdq_kv_shape *shape, int q_heads, int sequences, int max_new, int max_len);
 int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope, const svdq_kv_rows *q,

@@ -244,6 +244,7 @@ struct KvAttentionParams {
     int q_heads, group;      // group = q_heads / cache.heads
     float scale;             // of the scores, times log2(e)
     int causal, window;      // window = 0: none
+    int least_rows, most_rows;     // sequences with fewer rows a head are not for the many-row kernel, those with more not for the few-row kernel
     int tile_rows, parts;    // many-row kernel: rows of a workgroup (128 or 256), parts that the keys of a row tile are cut into
     int row_tiles;           // few-row kernel: tiles of 16 rows a sequence and head may need
     int row_cap;             // few-row kernel: rows that a tile can have

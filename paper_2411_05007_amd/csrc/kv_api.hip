@@ -91,7 +91,7 @@ int svdq_kv_append(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, c
 size_t svdq_kv_attention_workspace_bytes(const svdq_kv_shape *shape, int q_heads, int sequences, int max_new, int max_len) {
     if (!shape || check_shape(*shape) != SVDQ_OK || q_heads <= 0 || q_heads % shape->kv_heads != 0 || sequences < 0 || max_new < 0 || max_len < 0 || max_len > kMaxTokens)
         return 0;
-    return svdq::plan_kv_attention(sequences, shape->kv_heads, q_heads / shape->kv_heads, shape->head_dim, max_new, max_len, 0, false).total;
+    return svdq::plan_kv_attention(sequences, shape->kv_heads, q_heads / shape->kv_heads, shape->head_dim, max_new, max_len, 0, -1).total;
 }
 
 int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope, const svdq_kv_rows *q, int q_heads,
@@ -108,7 +108,8 @@ int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch
     if (!out || ((uintptr_t)out & 15) || !workspace || ((uintptr_t)workspace & 255)) return SVDQ_EINVAL;
     if (batch->max_len > kMaxTokens || (long long)batch->new_tokens * (q_heads / s.kv_heads) > 0x7fffffffll - (1 << 20)) return SVDQ_EUNSUPPORTED;
     const svdq::KvPlan plan = svdq::plan_kv_attention(batch->sequences, s.kv_heads, q_heads / s.kv_heads, s.head_dim, batch->max_new, batch->max_len, causal ? window : 0,
-                                                          batch->new_tokens == (long long)batch->sequences * batch->max_new);
+                                                          batch->new_tokens);
+    if (plan.few && (long long)batch->sequences * plan.row_tiles > kMaxGridY) return SVDQ_EUNSUPPORTED;
     if (workspace_bytes < plan.total) return SVDQ_ENOSPACE;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     svdq::KvAttentionParams p{};
@@ -123,22 +124,27 @@ int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch
     p.causal = causal != 0;
     p.window = window;
     p.tile_rows = plan.tile_rows;
-    p.parts = (long long)batch->new_tokens <= (long long)batch->sequences * batch->max_new ? plan.parts : 1;      // (the workspace has room for max_new of each)
+    p.parts = plan.parts;
     p.row_tiles = plan.row_tiles;
     p.row_cap = plan.row_cap;
     p.chunk_blocks = plan.chunk_blocks;
     p.chunks = plan.chunks;
     p.partial = reinterpret_cast<float *>(ws);
     p.part_ml = reinterpret_cast<float *>(ws + plan.ml_off);
-    p.arrived = reinterpret_cast<unsigned long long *>(ws + plan.words_off);
+    p.least_rows = plan.few ? svdq::kKvFewRows + 1 : 0;
+    p.most_rows = plan.many ? svdq::kKvFewRows : 0x7fffffff;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (!plan.few) {
+    if (plan.many) {
         const long long items = (long long)batch->new_tokens * p.group / plan.tile_rows + batch->sequences;
         if (items * s.kv_heads > 0x7fffffffll) return SVDQ_EUNSUPPORTED;
-        return done(svdq::launch_kv_attention_tile(p, stream));
+        const hipError_t e = svdq::launch_kv_attention_tile(p, stream);
+        if (e != hipSuccess) return done(e);
     }
-    if ((long long)batch->sequences * plan.row_tiles > kMaxGridY) return SVDQ_EUNSUPPORTED;
-    return plan.row_tiles == 0 ? SVDQ_OK : done(svdq::launch_kv_attention_rows(p, stream));
+    if (!plan.few || plan.row_tiles == 0) return SVDQ_OK;
+    // (after the other kernel: where that one adds parts, it adds them for every token of the batch)
+    p.partial = reinterpret_cast<float *>(ws + plan.few_off);
+    p.arrived = reinterpret_cast<unsigned long long *>(ws + plan.words_off);
+    return done(svdq::launch_kv_attention_rows(p, stream));
 }
 
 int svdq_kv_gather(const svdq_kv_cache_dev *cache, const int32_t *first_token, const int32_t *cu_rows, const int32_t *block_table, int sequences,

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     int t0, n;
     kv_range(p.batch.cu, b, p.batch.total, t0, n);
     const int len = __builtin_amdgcn_readfirstlane(kv_length(p.cache, p.batch, p.batch.kv_len[b])), rows = n * p.group;
-    if (tile * 16 >= rows) return;
+    if (tile * 16 >= rows || rows > p.most_rows) return;
     // the lane's row and the keys [seen_lo, seen_hi) that it sees
     const int r = tile * 16 + l16 < rows ? tile * 16 + l16 : rows - 1;
     const int tok = r / p.group, qh = head * p.group + r % p.group, pos = len - n + tok;

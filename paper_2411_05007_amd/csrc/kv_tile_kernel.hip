@@ -46,7 +46,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, h32 = lane >> 5;
     const int head = blockIdx.x % p.cache.heads, part = blockIdx.y;
-    const KvItem item = kv_item(p.batch, blockIdx.x / p.cache.heads, [&](int n, int) { return (n * p.group + kRows - 1) / kRows; });
+    const KvItem item = kv_item(p.batch, blockIdx.x / p.cache.heads, [&](int n, int) { return n * p.group < p.least_rows ? 0 : (n * p.group + kRows - 1) / kRows; });
     const int b = item.sequence, local = item.local, t0 = item.first, n = item.count;
     const int len = kv_length(p.cache, p.batch, item.value), rows = n * p.group, tiles = (rows + kRows - 1) / kRows;
     if (local < 0 || local >= tiles) return;

@@ -771,11 +771,13 @@ inline Workspace workspace_layout(int M, int K, int N, int rank, int ksplit_over
 constexpr unsigned long long kKvArrived = 0x4b56535644514152ull;      // as kActArrived: what a workgroup leaves in its arrival word
 constexpr int kKvMostChunks = 256;
 struct KvPlan {
-    bool few;                                          // the kernel of sixteen rows a workgroup (kv_rows_kernel.hip), or of 128 or 256 (kv_tile_kernel.hip)
+    bool few, many;                                    // the kernel of sixteen rows a workgroup (kv_rows_kernel.hip), the one of 128 or 256 (kv_tile_kernel.hip), or each for its sequences
     int row_tiles, row_cap, chunk_blocks, chunks;      // few
     int tile_rows, parts;                              // many
-    size_t words_off, ml_off, total;                   // bytes of the workspace (partial sums lie at its start)
+    size_t ml_off, few_off, words_off, total;          // bytes of the workspace: partial sums of many at its start, their maxima and sums, the same of few, arrival words
 };
+// Sequences of so many rows go to the kernel of few where a batch takes both.
+constexpr int kKvFewRows = 16;
 // Few: blocks of 32 keys of a chunk, for `blocks` of them in the longest sequence and `wgs` row tiles of all heads and sequences.  A workgroup costs 5 us
 // beside its blocks (0.15 us each while its CU is alone with it) and parts that meet 4.5 us more: one token on 1024 keys of eight heads takes 10.3 us whole
 // and 10.7 in pieces of 8 blocks, on 2048 keys 15.3 and 10.8.  So keys of at most 32 blocks stay whole; others are cut until there is a workgroup
@@ -814,27 +816,7 @@ inline bool kv_few_rows(int sequences, int heads, int dim, long long rows, int m
     const double many = 15000.0 + (parts > 1 ? 12000.0 : 0.0) + (rounds > 1.0 ? rounds : 1.0) * 2200.0 * (double)max_len / 64.0 / parts * dim / 128.0;
     return few <= many;
 }
-// window: 0 or the keys that a row sees; it does not change the kernel, and asks for no more workspace than none.  even: all sequences have max_new tokens.
-inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len, int window, bool even) {
-    KvPlan p{};
-    const long long rows = (long long)max_new * group;
-    p.few = kv_few_rows(sequences, heads, dim, rows, max_len);
-    p.chunks = p.parts = 1;
-    p.total = 256;
-    if (!p.few) {
-        // 256 rows, one workgroup on a CU, stage a tile of keys for twice the rows: 8192 tokens x 4 heads on 16384 keys 1539 us (128 rows: 1618), joint attention of 4608
-        // tokens 281 (300); but what is masked or left over is larger: ragged chunks 357 (355), 7409 rows x 2 in a window 498 (469).
-        const long long large = (long long)sequences * ((rows + 255) / 256) * heads, small = (long long)sequences * ((rows + 127) / 128) * heads;
-        p.tile_rows = dim == 128 && even && window == 0 && max_len >= 4096 && large >= 256 ? 256 : 128;
-        const long long keys = window > 0 && (long long)window + 128 / group < max_len ? (long long)window + 128 / group : max_len;
-        p.parts = p.tile_rows == 256 ? 1 : kv_parts(small, dim == 256 ? 256 : 512, keys);
-        if (p.parts > 1) {
-            const size_t all = (size_t)p.parts * sequences * max_new * heads * group;
-            p.ml_off = align256(all * dim * 4);
-            p.total = p.ml_off + align256(all * 8);
-        }
-        return p;
-    }
+inline void plan_kv_rows(KvPlan &p, int sequences, int heads, int dim, long long rows, int max_new, int max_len, int window) {
     p.row_tiles = (int)((rows + 15) / 16);
     p.row_cap = rows < 16 ? (int)rows : 16;
     const long long wgs = (long long)sequences * heads * p.row_tiles;
@@ -843,7 +825,8 @@ inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, in
     p.chunks = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
     if (p.chunks > 1) {
         const size_t parts = (size_t)sequences * p.row_tiles * heads * p.chunks;
-        p.words_off = align256(parts * p.row_cap * (dim + 2) * 4);
+        p.few_off = p.total;
+        p.words_off = p.few_off + align256(parts * p.row_cap * (dim + 2) * 4);
         p.total = p.words_off + align256(parts * 8);
     }
     if (window > 0 && ((long long)window + max_new) / 32 + 2 < blocks) {      // no more chunks than the workspace has room for
@@ -852,6 +835,46 @@ inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, in
         p.chunk_blocks = c > least ? c : least;
         p.chunks = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
     }
+}
+// tokens: new ones of all sequences, -1 if they are not known yet (the workspace for any number of them).  window: 0 or the keys that a row sees.  Neither changes
+// the kernel of the longest sequence, and a call needs no more workspace than without them.
+inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len, int window, long long tokens) {
+    KvPlan p{};
+    const long long rows = (long long)max_new * group, most_tokens = (long long)sequences * max_new;
+    p.few = kv_few_rows(sequences, heads, dim, rows, max_len);
+    p.many = !p.few;
+    p.chunks = p.parts = 1;
+    if (p.few) {
+        plan_kv_rows(p, sequences, heads, dim, rows, max_new, max_len, window);
+        p.total = p.total < 256 ? 256 : p.total;
+        return p;
+    }
+    // 256 rows, one workgroup on a CU, stage a tile of keys for twice the rows: 8192 tokens x 4 heads on 16384 keys 1530 us (128 rows: 1618), joint attention of 4608
+    // tokens 278 (300), whole prompts of 4096 336 (332); what is masked or left over is larger, though: whole prompts of 2048 226 (212), ragged chunks 357 (355), 7409
+    // rows x 2 in a window 498 (469).
+    const long long slots = dim == 256 ? 256 : 512, large = (long long)sequences * ((rows + 255) / 256) * heads;
+    p.tile_rows = dim == 128 && tokens == most_tokens && window == 0 && max_len >= 4096 && large >= 256 ? 256 : 128;
+    const long long keys = window > 0 && (long long)window + 128 / group < max_len ? (long long)window + 128 / group : max_len;
+    if (p.tile_rows == 128 && tokens >= 0 && tokens <= most_tokens) {
+        const long long tiles = tokens * group / 128 + sequences, even = sequences * ((rows + 127) / 128);      // at most so many
+        p.parts = kv_parts((tiles < even ? tiles : even) * heads, slots, keys);
+    }
+    const double most = 16.0 * (double)most_tokens * group * heads;      // (parts x row tiles are no more than `slots`, and parts no more than 16)
+    const size_t all = tokens >= 0 ? (size_t)p.parts * tokens * heads * group : most < (double)(slots * 128) ? (size_t)most : (size_t)slots * 128;
+    if (tokens >= 0 ? p.parts > 1 : kv_parts(1, slots, keys) > 1) {
+        p.ml_off = align256(all * dim * 4);
+        p.total = p.ml_off + align256(all * 8);
+    }
+    // A batch may hold chunks of prompts beside single tokens, whose many keys one workgroup of 128 rows would walk alone.  Where the mean sequence has well under the most
+    // tokens, those of at most sixteen rows go to the kernel of few.  Together | so (8 key heads of 128, 32 query heads): 512 tokens on 4512 beside seven single ones on
+    // 32000 keys 623 us | 148, beside three on 100000 1935 | 166, beside 31 on 8000 195 | 163; 2048 on 4096 beside 31 on 4000 196 | 146; 256 beside 63 on 2000 63 | 40;
+    // a batch without such a sequence pays 1.5 us for the launch.
+    if (sequences > 1 && group <= kKvFewRows && 5 * tokens < 3 * most_tokens) {
+        p.few = true;
+        const long long few_rows = rows < kKvFewRows ? rows : kKvFewRows;
+        plan_kv_rows(p, sequences, heads, dim, few_rows, (int)(few_rows / group), max_len, window);
+    }
+    p.total = p.total < 256 ? 256 : p.total;
     return p;
 }
 

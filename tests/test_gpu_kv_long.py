@@ -172,6 +172,21 @@ def test_keys_in_parts(torch, KV, dim, heads, group, new, lens, causal, window, 
     check(torch, KV, pool, rng, group, shared(rng, pool, lens, holes), lens, new, causal, window, turn(torch, KV, max(lens), dim, True), extra=extra)
 
 
+@pytest.mark.parametrize("dim,heads,group,new,lens,causal,window,extra", [
+    (128, 2, 4, [300, 1, 4, 5, 0, 1], [8000, 7000, 4, 900, 0, 1], True, 0, 0),        # with parts of the chunk's keys; 16 rows and 20
+    (128, 8, 4, [1] * 20 + [512] + [2] * 11, [8000] * 20 + [512] + [777] * 11, True, 0, 4),
+    (64, 3, 8, [1, 2, 3, 700, 1], [12000, 5000, 40, 12000, 1], True, 500, 0),
+    (64, 12, 1, [400, 16, 17, 1, 399, 15, 1, 1], [3000, 16, 2000, 3000, 399, 64, 65, 1], False, 0, 0),
+    (256, 2, 2, [600, 1, 8, 9, 1], [3000, 2999, 600, 3000, 33], True, 0, 2),
+    (128, 2, 17, [300, 1, 1, 8], [8000, 7999, 5, 64], True, 0, 0),                       # a single token is two tiles of rows
+])
+@pytest.mark.parametrize("holes", [False, True])
+def test_chunks_beside_single_tokens(torch, KV, dim, heads, group, new, lens, causal, window, extra, holes):
+    rng = np.random.default_rng(dim + len(new))
+    pool = Pool(torch, KV, heads, dim, 64, 140, 27)
+    check(torch, KV, pool, rng, group, shared(rng, pool, lens, holes), lens, new, causal, window, turn(torch, KV, max(lens), dim // 2, False), extra=extra, samples=60)
+
+
 @pytest.mark.parametrize("heads,group,new,length", [(8, 1, 256, 4200), (8, 2, 150, 2000), (2, 4, 300, 8000)])
 def test_a_key_that_is_not_finite_reaches_the_rows_that_see_it(torch, KV, heads, group, new, length):
     rng = np.random.default_rng(heads + new)
