@@ -3,13 +3,18 @@
 //   O_i = sum_j softmax_j(scale q'_i . k_j) v_j,   q' the rotated query, j over the keys that row i sees.
 //
 // The rows of a sequence and key head are its new tokens times the query heads that share the head, so a tile of keys serves the whole group.  A
-// workgroup of four wavefronts has 128 rows, 32 to a wavefront; keys and values go by in tiles of 64 tokens, read once per workgroup as codes,
-// converted to f16 on the way into LDS (exact: codes of the keys, code * 2^(byte - reference) of the values, the reference exponent the largest seen)
-// and laid out as operands, so that an operand read is 64 lanes x 16 bytes in a row.  S^T = K Q^T by v_mfma_f32_32x32x16_f16: a lane has one row of
-// queries, its accumulators are the operand of O^T = V^T P^T as they stand, and maximum and sum of a row are one exchange between lane
-// halves away.  Statistics in fp32; P is exp2(t - m + 8) in f16, at most 2^14 before the maximum is renewed, so weights down to 2^-22 of the
-// largest keep eleven bits; Q in f16, scaled by a power of two per row.
-// Bound: the exponentials and the matrix products take turns (per 64 tokens and wavefront 32 matrix instructions and about 250 vector ones).
+// workgroup has 128 rows (four wavefronts, two workgroups on a CU) or 256 (eight, one; head size 128, long even batches), 32 to a wavefront; keys and values go by
+// in tiles of 64 tokens, read once per workgroup as codes, converted to f16 on the way into LDS (exact: codes of the keys, code * 2^(byte - reference) of the values, the
+// reference exponent the largest seen) and laid out as operands, so that an operand read is 64 lanes x 16 bytes in a row.  S^T = K Q^T by
+// v_mfma_f32_32x32x16_f16: a lane has one row of queries, its accumulators are the operand of O^T = V^T P^T as they stand, and maximum and sum of a row are one exchange
+// between lane halves away.  Statistics in fp32; P is exp2(t - m + 8) in f16, at most 2^14 before the maximum is renewed, so weights down to 2^-22 of the
+// largest keep eleven bits; Q in f16, scaled by a power of two per row, for the same eleven bits.
+// The scores of a tile are made beside the weights of the one before, codes are requested two and three tiles ahead, pages and scale bytes 32 tiles ahead; one barrier a tile.
+// Few row tiles on many keys take parts of the keys, which kv_meet_kernel adds.  A wavefront whose rows are past the sequence's only carries codes.
+// Bound: matrix cores and vector ALU, which overlap little, at the chip's power limit (2.05 of 2.4 GHz).  8192 tokens, 32 query heads on 8, on 16384 keys 1530 us, 1.08 PFLOP/s
+// (a library product of 8192 cubed in f16 reaches 1.215): matrix cores busy 52 % of the time, vector ALU 55 %; 4608 tokens of 24 heads, all with all, 279 us, 49 and 54 %, and 432
+// tiles are two rounds of 256 CUs; six ragged chunks of up to 2111 tokens 355 us, 43 and 57 %.  What a workgroup of 128 rows costs beside its tiles (1.05 us each): scan over
+// the sequences 1.2 us, queries and first pages 2.2, turning 2.5, first codes 1.4, out 2, of which the other workgroup of the CU covers about two thirds.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <type_traits>
