@@ -115,16 +115,23 @@ class KVCache:
     def _stream(self, stream):
         return _current_stream(self.device.index) if stream is None else stream.cuda_stream
 
+    def _new(self, shape, dtype, stream):
+        """Memory of the current stream that a call on `stream` writes: not given out again before that stream is done with it."""
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        if stream is not None:
+            t.record_stream(stream)
+        return t
+
     def append(self, k, v, batch: KVBatch, rope: Optional[Rope] = None, stream=None) -> None:
         """k, v: bf16 [new_tokens, kv_heads, head_dim] (any token and head stride that keeps 16-byte alignment)."""
         kd, vd = self._rows(k, self.kv_heads, batch.new_tokens, "k"), self._rows(v, self.kv_heads, batch.new_tokens, "v")
         S._check(S.lib().svdq_kv_append(self.cdesc, batch.cdesc, None if rope is None else rope.cdesc, kd, vd, self._stream(stream)), "svdq_kv_append")
 
-    def attention_workspace(self, batch: KVBatch, q_heads: int):
+    def attention_workspace(self, batch: KVBatch, q_heads: int, stream=None):
         n = S.lib().svdq_kv_attention_workspace_bytes(C.byref(self.shape), int(q_heads), batch.sequences, batch.max_new, batch.max_len)
         if n == 0:
             raise S.SvdqError("unsupported shape")
-        return torch.empty(n, dtype=torch.uint8, device=self.device)
+        return self._new(n, torch.uint8, stream)
 
     def attention(self, q, batch: KVBatch, rope: Optional[Rope] = None, scale: Optional[float] = None, causal: bool = True, window: int = 0,
                   out=None, workspace=None, stream=None):
@@ -132,11 +139,13 @@ class KVCache:
         qd = self._rows(q, None, batch.new_tokens, "q")
         heads = q.shape[1]
         if out is None:
-            out = torch.empty((batch.new_tokens, heads, self.head_dim), dtype=torch.bfloat16, device=q.device)
+            out = self._new((batch.new_tokens, heads, self.head_dim), torch.bfloat16, stream)
         else:
             assert out.dtype is torch.bfloat16 and out.is_cuda and out.is_contiguous() and out.shape == q.shape
         if workspace is None:
-            workspace = self.attention_workspace(batch, heads)
+            workspace = self.attention_workspace(batch, heads, stream)
+        else:
+            assert workspace.dtype is torch.uint8 and workspace.is_cuda and workspace.is_contiguous(), "workspace: uint8 on the GPU"
         S._check(S.lib().svdq_kv_attention(self.cdesc, batch.cdesc, None if rope is None else rope.cdesc, qd, heads,
                                            1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(causal), int(window), out.data_ptr(),
                                            workspace.data_ptr(), workspace.numel(), self._stream(stream)), "svdq_kv_attention")
@@ -146,7 +155,7 @@ class KVCache:
         """Keys and values bf16 [rows, kv_heads, head_dim] as they are held."""
         shape = (rows.rows, self.kv_heads, self.head_dim)
         if out is None:
-            out = [torch.empty(shape, dtype=torch.bfloat16, device=self.device) for _ in range(2)]
+            out = [self._new(shape, torch.bfloat16, stream) for _ in range(2)]
         for t in out:
             assert t.dtype is torch.bfloat16 and t.is_cuda and t.is_contiguous() and t.shape == shape
         S._check(S.lib().svdq_kv_gather(self.cdesc, *rows.pointers, rows.sequences, rows.width, rows.rows, out[0].data_ptr(), out[1].data_ptr(), self._stream(stream)),

@@ -242,6 +242,35 @@ def test_lengths_far_past_the_bound(torch, KV, new, bound):
     check(torch, KV, pool, rng, 4, shared(rng, pool, lens), lens, [new] * 3, True, 0, max_len=bound, samples=15)
 
 
+def test_memory_that_a_call_allocates_for_another_stream_stays_its_own(torch, KV):
+    """The workspace is the binding's, on the current stream; its next owner there must not write to it while the call's stream is still to run."""
+    rng = np.random.default_rng(4)
+    pool = Pool(torch, KV, 2, 128, 64, 60, 29)
+    lens = [9000, 5000]
+    table = i32(torch, shared(rng, pool, lens))
+    q = torch.randn(2, 8, 128, device=DEV).to(torch.bfloat16)
+    batch = KV.KVBatch(i32(torch, [0, 1, 2]), i32(torch, lens), table, 2, 1, 9000)
+    want = pool.cache.attention(q, batch)
+    n = pool.cache.attention_workspace(batch, 8).numel()
+    assert n > 4096      # (parts that meet)
+    rows = KV.KVRows(i32(torch, [0]), i32(torch, [0, 9000]), table[:1].contiguous(), 9000)
+    kv = pool.cache.gather(rows)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device=DEV)
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            for _ in range(4):
+                big @ big      # (the side stream is busy for a while)
+        got = pool.cache.attention(q, batch, stream=side)
+        mine = [torch.full((n,), 0x41, dtype=torch.uint8, device=DEV) for _ in range(4)]
+        k, v = pool.cache.gather(rows, stream=side)
+        mine += [torch.full((9000, 2, 128), 3.0, dtype=torch.bfloat16, device=DEV) for _ in range(4)]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(k, kv[0]) and torch.equal(v, kv[1])
+        del got, k, v, mine
+
+
 # ---- append and gather ----------------------------------------------------------------------------------------------------------------------
 
 
@@ -312,3 +341,15 @@ def test_strides_the_entry_points_refuse(torch, KV):
     x = torch.zeros(64, dtype=torch.bfloat16, device=DEV)
     with pytest.raises(S.SvdqError, match="unsupported"):
         cache.append(torch.as_strided(x, (1, 1, 64), ((1 << 25) + 8, 64, 1)), torch.as_strided(x, (1, 1, 64), (64, 64, 1)), batch)
+
+
+def test_workspaces_that_are_refused(torch, KV):
+    cache = KV.KVCache(2, 1, 64, 32)
+    batch = KV.KVBatch(i32(torch, [0, 1]), i32(torch, [1]), i32(torch, [[0]]), 1, 1, 1)
+    q = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device=DEV)
+    for bad in (torch.zeros(256, dtype=torch.uint8), torch.zeros(64, dtype=torch.float32, device=DEV), torch.zeros(512, dtype=torch.uint8, device=DEV)[::2]):
+        with pytest.raises(AssertionError):
+            cache.attention(q, batch, workspace=bad)
+    for bad in (torch.zeros(128, dtype=torch.uint8, device=DEV), torch.zeros(1024, dtype=torch.uint8, device=DEV)[16:]):
+        with pytest.raises(S.SvdqError):
+            cache.attention(q, batch, workspace=bad)
