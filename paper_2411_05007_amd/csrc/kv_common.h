@@ -60,7 +60,8 @@ __device__ __forceinline__ KvItem kv_item(const KvBatch &t, int item, Units unit
         if (past != 0ull) {
             const int at = __builtin_ctzll(past);
             got.sequence = b0 + at;
-            got.local = item - __builtin_amdgcn_readlane(upto - mine, at);
+            const int local = item - __builtin_amdgcn_readlane(upto - mine, at);
+            got.local = (uint32_t)local < (uint32_t)__builtin_amdgcn_readlane(mine, at) ? local : -1;      // (counts that do not ascend may sum past 32 bits)
             got.first = __builtin_amdgcn_readlane(first, at);
             got.count = __builtin_amdgcn_readlane(count, at);
             got.value = __builtin_amdgcn_readlane(value, at);
