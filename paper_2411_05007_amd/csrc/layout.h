@@ -855,8 +855,11 @@ inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, in
     const long long slots = dim == 256 ? 256 : 512, large = (long long)sequences * ((rows + 255) / 256) * heads;
     p.tile_rows = dim == 128 && tokens == most_tokens && window == 0 && max_len >= 4096 && large >= 256 ? 256 : 128;
     const long long keys = window > 0 && (long long)window + 128 / group < max_len ? (long long)window + 128 / group : max_len;
+    // Does the batch hold chunks beside single tokens?  Where the mean sequence has less than a third of the most tokens, or all but one have sixteen rows in the mean.
+    const bool mixed = sequences > 1 && group <= kKvFewRows && (10 * tokens < 3 * most_tokens || (tokens - max_new) * group <= (long long)kKvFewRows * (sequences - 1));
+    const long long large_ones = mixed && max_new > 0 ? (tokens + max_new - 1) / max_new : sequences;
     if (p.tile_rows == 128 && tokens >= 0 && tokens <= most_tokens) {
-        const long long tiles = tokens * group / 128 + sequences, even = sequences * ((rows + 127) / 128);      // at most so many
+        const long long tiles = tokens * group / 128 + large_ones, even = sequences * ((rows + 127) / 128);      // at most so many, but for single tokens
         p.parts = kv_parts((tiles < even ? tiles : even) * heads, slots, keys);
     }
     const double most = 16.0 * (double)most_tokens * group * heads;      // (parts x row tiles are no more than `slots`, and parts no more than 16)
@@ -865,11 +868,14 @@ inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, in
         p.ml_off = align256(all * dim * 4);
         p.total = p.ml_off + align256(all * 8);
     }
-    // A batch may hold chunks of prompts beside single tokens, whose many keys one workgroup of 128 rows would walk alone.  Where the mean sequence has well under the most
-    // tokens, those of at most sixteen rows go to the kernel of few.  Together | so (8 key heads of 128, 32 query heads): 512 tokens on 4512 beside seven single ones on
-    // 32000 keys 623 us | 148, beside three on 100000 1935 | 166, beside 31 on 8000 195 | 163; 2048 on 4096 beside 31 on 4000 196 | 146; 256 beside 63 on 2000 63 | 40;
-    // a batch without such a sequence pays 1.5 us for the launch.
-    if (sequences > 1 && group <= kKvFewRows && 5 * tokens < 3 * most_tokens) {
+    // Single tokens beside chunks go to the kernel of few, in a launch of their own, where that is estimated to cost less (us; a row tile costs a CU 5 and 1.05 for 64 keys), or
+    // where a lone workgroup would walk the longest sequence for 60 us.  Together | apart, us (8 key heads of 128, 32 query heads): 512 tokens on 4512 beside seven single
+    // ones on 32000 keys 623 | 137, beside three on 100000 1935 | 166, beside 31 on 16000 350 | 194, beside seven on 1500 63 | 78; 256 beside 63 on 500 32 | 26, on 4000
+    // 106 | 69; 2048 on 2048 beside 31 on 4000 131 | 83, on 500 59 | 68.  Not mixed: 64 sequences of 1 to 16 tokens on up to 4000 keys 100 | 149.
+    const double tile_us = 5.0 + 1.05 * (double)keys / 64.0 * dim / 128.0, rounds = (double)tokens * group / 128.0 * heads / 256.0;
+    const double together = (rounds + (double)sequences * heads / 256.0) * tile_us;
+    const double apart = (rounds + (double)large_ones * heads / 256.0) * tile_us + 10.0 + 0.75e-3 * sequences * heads * (double)keys / 32.0 * dim / 128.0;
+    if (mixed && (tokens < 0 || apart < together || tile_us / p.parts > 60.0)) {
         p.few = true;
         const long long few_rows = rows < kKvFewRows ? rows : kKvFewRows;
         plan_kv_rows(p, sequences, heads, dim, few_rows, (int)(few_rows / group), max_len, window);

@@ -179,6 +179,11 @@ def test_keys_in_parts(torch, KV, dim, heads, group, new, lens, causal, window, 
     (64, 12, 1, [400, 16, 17, 1, 399, 15, 1, 1], [3000, 16, 2000, 3000, 399, 64, 65, 1], False, 0, 0),
     (256, 2, 2, [600, 1, 8, 9, 1], [3000, 2999, 600, 3000, 33], True, 0, 2),
     (128, 2, 17, [300, 1, 1, 8], [8000, 7999, 5, 64], True, 0, 0),                       # a single token is two tiles of rows
+    # the single tokens in a launch of their own
+    (64, 12, 1, [400] + [16] * 20 + [17] * 2 + [1] * 40, [3000] + [2900, 16] * 10 + [17, 1700] + [1, 3000, 33, 640] * 10, True, 0, 3),
+    (256, 2, 2, [1] * 15 + [600] + [1] * 15 + [8, 9], [2999, 1, 700] * 5 + [3000] + [64, 2048, 33] * 5 + [8, 2000], True, 0, 0),
+    (128, 8, 8, [1] * 30 + [700], [9000, 1, 3100] * 10 + [8999], True, 3000, 0),
+    (128, 8, 4, [512, 1], [4000, 100000], True, 0, 0),
 ])
 @pytest.mark.parametrize("holes", [False, True])
 def test_chunks_beside_single_tokens(torch, KV, dim, heads, group, new, lens, causal, window, extra, holes):

@@ -92,9 +92,10 @@ def test_plans_stay_within_the_workspace_and_the_kernels_bounds(plan):
     (64, 8, 4, 128, 1, 500, 0, 64, "few 1"), (1, 1, 4, 128, 1, 5001, 0, 1, "few 20"), (1, 1, 4, 64, 1, 2201600, 0, 1, "few 256"),
     (32, 8, 1, 128, 256, 4200, 0, 8192, "256 1"), (4, 4, 2, 128, 4100, 4100, 0, 16400, "256 1"),
     (24, 8, 2, 128, 199, 2800, 0, 3300, "128 1"), (24, 12, 1, 64, 399, 2999, 65, 7000, "128 1"), (40, 2, 4, 256, 199, 2799, 0, 5000, "128 1"),
-    (2, 2, 4, 128, 300, 8000, 0, 600, "128 12"), (2, 2, 4, 128, 300, 8000, 0, 337, "128 15, few 32"), (1, 1, 8, 128, 2000, 2000, 0, 2000, "128 3"),
+    (2, 2, 4, 128, 300, 8000, 0, 600, "128 12"), (2, 2, 4, 128, 300, 8000, 0, 337, "128 15"), (1, 1, 8, 128, 2000, 2000, 0, 2000, "128 3"),
     (2, 3, 4, 64, 700, 12000, 0, 1350, "128 3"), (6, 2, 2, 256, 600, 3000, 0, 3600, "128 2"), (150, 4, 2, 128, 60, 659, 0, 5400, "128 1"),
-    (16, 4, 2, 128, 200, 3000, 0, 3200, "128 2"), (32, 8, 4, 128, 512, 8000, 0, 543, "128 1, few 2"), (4, 2, 17, 128, 300, 8000, 0, 310, "128 5"),
+    (16, 4, 2, 128, 200, 3000, 0, 3200, "128 2"), (32, 8, 4, 128, 512, 8000, 0, 554, "128 3, few 2"), (63, 12, 1, 64, 400, 3000, 0, 794, "128 5, few 1"),
+    (33, 2, 2, 256, 600, 3000, 0, 647, "128 5, few 3"), (31, 8, 8, 128, 700, 9000, 3000, 730, "128 1, few 1"), (2, 8, 4, 128, 512, 100000, 0, 513, "128 3, few 25"), (4, 2, 17, 128, 300, 8000, 0, 310, "128 5"),
 ])
 def test_the_kernels_that_the_gpu_tests_reach(plan, sequences, heads, group, dim, max_new, max_len, window, tokens, want):
     assert plan(sequences, heads, group, dim, max_new, max_len, window, tokens).stdout.strip() == want
