@@ -141,7 +141,7 @@ int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch
         if (e != hipSuccess) return done(e);
     }
     if (!plan.few || plan.row_tiles == 0) return SVDQ_OK;
-    // (after the other kernel: where that one adds parts, it adds them for every token of the batch)
+    // (behind the other kernel: where that one's parts are added, it is for every token of the batch, and what it makes of those without parts is written over here)
     p.partial = reinterpret_cast<float *>(ws + plan.few_off);
     p.arrived = reinterpret_cast<unsigned long long *>(ws + plan.words_off);
     return done(svdq::launch_kv_attention_rows(p, stream));
