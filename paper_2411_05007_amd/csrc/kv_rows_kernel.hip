@@ -28,7 +28,7 @@
 namespace svdq {
 namespace {
 
-constexpr float kNone = -1e30f;                  // the running maximum before the first key
+constexpr float kNone = -3.4028235e38f;          // the running maximum before the first key: the lowest number, so that any score of a key that is seen renews it
 constexpr float kShift = 8.f, kSlack = 6.f;      // P is exp2(t - m + kShift); m is renewed when a score passes it by kSlack
 constexpr int WAVES = 4;
 

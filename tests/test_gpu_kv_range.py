@@ -1,0 +1,80 @@
+"""Attention over the paged 8-bit cache at the ends of the range: scores and values as large or as small as 16-bit inputs make them, in both kernels.  The content is read
+back by gather, and rows are compared with 64 bits over the keys that they see; what a row does not see must not matter to it."""
+import numpy as np
+import pytest
+
+from paper_2411_05007_amd import svdq as S
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+# new tokens of a sequence and how often the batch holds it: single tokens (the kernel of few rows), and so many rows that the kernel of many takes them
+FEW, MANY = (1, 1), (200, 256)
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    assert t.cuda.is_available(), "these tests need the MI355X"
+    S.lib()
+    return t
+
+
+@pytest.fixture(scope="module")
+def KV(torch):
+    from paper_2411_05007_amd import kv
+    return kv
+
+
+class Sequence:
+    """Keys and values fp32 [L, heads, D] in a cache, and what it holds of them in 64 bits."""
+
+    def __init__(self, torch, KV, k, v, page=64):
+        self.torch, self.KV = torch, KV
+        self.L, self.heads, self.D = k.shape
+        pages = (self.L + page - 1) // page
+        self.cache = KV.KVCache(pages, self.heads, self.D, page)
+        self.table = torch.arange(pages, dtype=torch.int32, device=DEV)[None].contiguous()
+        self.cache.append(k.to(DEV).to(torch.bfloat16), v.to(DEV).to(torch.bfloat16), KV.KVBatch(self.i32([0, self.L]), self.i32([self.L]), self.table, self.L, self.L, self.L))
+        self.k, self.v = (t.double().cpu() for t in self.cache.gather(KV.KVRows(self.i32([0]), self.i32([0, self.L]), self.table, self.L)))
+
+    def i32(self, x):
+        return self.torch.tensor(np.asarray(x), dtype=self.torch.int32, device=DEV)
+
+    def attend(self, q, copies=1, length=None, max_new=None, **kw):
+        """q fp32 [new, q_heads, D], the sequence's last tokens, in a batch that holds it `copies` times; fp64 [new, q_heads, D]"""
+        torch, new, length = self.torch, q.shape[0], self.L if length is None else length
+        q = q.to(DEV).to(torch.bfloat16)
+        batch = self.KV.KVBatch(self.i32(np.arange(copies + 1) * new), self.i32([length] * copies), self.table.expand(copies, -1).contiguous(), new * copies,
+                                new if max_new is None else max_new, length)
+        out = torch.full((new * copies, q.shape[1], self.D), 7.0, dtype=torch.bfloat16, device=DEV)
+        out = self.cache.attention(q.repeat(copies, 1, 1), batch, out=out, **kw).view(copies, *q.shape)
+        assert torch.equal(out[0].view(torch.int16), out[copies - 1].view(torch.int16))
+        return out[copies // 2].double().cpu(), q.double().cpu()
+
+    def seen(self, i, new, causal=True, window=0):
+        pos = self.L - new + i
+        return slice(max(0, pos + 1 - window) if causal and window else 0, pos + 1 if causal else self.L)
+
+    def want(self, q, i, h, causal=True, window=0, scale=None):
+        """row i and head h of the output, and the weighted sum of magnitudes"""
+        keys, kh = self.seen(i, q.shape[0], causal, window), h // (q.shape[1] // self.heads)
+        p = self.torch.softmax(self.k[keys, kh] @ q[i, h] * (self.D ** -0.5 if scale is None else scale), 0)
+        return p @ self.v[keys, kh], p @ self.v[keys, kh].abs()
+
+
+def normal(torch, seed, *shape):
+    gen = torch.Generator()
+    gen.manual_seed(seed)
+    return torch.randn(*shape, generator=gen)
+
+
+@pytest.mark.parametrize("new,copies", [FEW, MANY])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_scores_near_the_lowest_number_are_scores(torch, KV, dim, new, copies):
+    """Every key the same, every score -2^100 sqrt(dim) (of powers of two, so that they are exact): the mean of the values."""
+    w = Sequence(torch, KV, torch.full((300, 1, dim), 2.0 ** 50), normal(torch, dim, 300, 1, dim))
+    got, _ = w.attend(torch.full((new, 2, dim), -2.0 ** 50), copies)
+    for i in {0, new - 1}:
+        v = w.v[w.seen(i, new), 0]
+        # equal weights are exact; fp32 sums of 300 products, a bf16 output
+        assert ((got[i] - v.mean(0)).abs() <= 2.0 ** -8 * v.mean(0).abs() + 2.0 ** -14 * v.abs().mean(0)).all()
