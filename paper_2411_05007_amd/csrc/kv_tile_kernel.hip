@@ -29,6 +29,7 @@ namespace {
 
 constexpr float kNone = -3.4028235e38f;          // the running maximum before the first key: the lowest number, so that any score of a key that is seen renews it
 constexpr float kShift = 8.f, kSlack = 6.f;      // P is exp2(t - m + kShift); m is renewed when a score passes it by kSlack
+constexpr float kFar = 16777216.f;               // exponents past it (2^24) have steps of two and more
 constexpr int kTileKeys = 64;
 
 // LDS of a tile of 64 keys as operands: of the keys step c, lane half h, token; of the values run a of 32 channels, slot g, channel.  The pads spread what
@@ -245,7 +246,8 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     float m = kNone, l = 0.f;
     int ref = 0;                   // byte of the reference scale of the values in o
     float kf[2];                   // factors of the scores that weight_pair() takes
-    float base;                    // kShift - m
+    bool far = false;              // a row's maximum is past kFar, or was
+    float base;                    // kShift - m; kShift where the scores have lost m already
     kv_f16x8 pf[4];
     typedef kv_floatx16 Scores[2];
 
@@ -290,6 +292,19 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
 #pragma unroll
             for (int a = 0; a < A; ++a) o[a] *= keep;
             m = m_new;
+            far = far || __builtin_amdgcn_ballot_w64(!(__builtin_fabsf(m) <= kFar) && most != -__builtin_inff()) != 0ull;
+        }
+        base = kShift - m;
+        // weight_pair() adds m to the product before it is rounded, but m is a rounded product, and kShift is lost beside a large one: once a maximum is far out, scores
+        // become their rounded distances to it here, so that the largest is zero as it should be (and NaN where it passed fp32)
+        if (far) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[i][v] = s[i][v] * kf[i] - m;
+                kf[i] = 1.f;
+            }
+            base = kShift;
         }
     };
     auto weight_pair = [&](const Scores &s, int q) {      // pair q of 16: two weights, and their sum
@@ -372,7 +387,6 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         auto step = [&](Scores &now, Scores &next, uint4 (&kn)[N], uint4 (&vn)[N], int t, auto partial) {      // kn: keys t + 2, vn: values t + 1
             const int held = refer(f1) > ref ? refer(f1) : ref;      // the scale that the next values in LDS refer to
             const unsigned char *keys = kt(t + 1), *values = vt(t);
-            base = kShift - m;
             clear_unnamed(vn, f1);
             if (APART) __builtin_amdgcn_s_setprio(1);
             kv_f16x8 kop[2][2], vop[4];
@@ -441,7 +455,6 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
                 even[1] = odd[1];
             }
         }
-        base = kShift - m;
 #pragma unroll
         for (int q = 0; q < 16; ++q) weight_pair(even, q);
 #pragma unroll

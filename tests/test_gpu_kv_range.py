@@ -78,3 +78,47 @@ def test_scores_near_the_lowest_number_are_scores(torch, KV, dim, new, copies):
         v = w.v[w.seen(i, new), 0]
         # equal weights are exact; fp32 sums of 300 products, a bf16 output
         assert ((got[i] - v.mean(0)).abs() <= 2.0 ** -8 * v.mean(0).abs() + 2.0 ** -14 * v.abs().mean(0)).all()
+
+
+@pytest.mark.parametrize("new,copies", [FEW, MANY, (300, 1)])
+@pytest.mark.parametrize("dim,size", [(64, 2.0 ** 12), (64, 2.0 ** 16), (128, 2.0 ** 14), (128, 2.0 ** 21), (128, 2.0 ** 40), (256, 2.0 ** 17)])
+def test_scores_of_any_size_have_a_largest(torch, KV, dim, size, new, copies):
+    """Scores of about 16 size^2.  Queries without a rotation are exact in f16 and codes are exact, so a score is off by the fp32 sum of its products alone, 2^-16 of their
+    magnitudes: where the second largest is farther than that and 40 below the largest, the row is the value of its largest key, rounded to 16 bits."""
+    L = 9000 if new == 300 else 300      # (300 rows on so many keys: in parts)
+    w = Sequence(torch, KV, normal(torch, 1, L, 1, dim) * size, normal(torch, 2, L, 1, dim))
+    got, q = w.attend(normal(torch, 3, new, 2, dim) * size, copies)
+    checked = 0
+    for i in {0, 1, new // 2, new - 1} & set(range(new)):
+        for h in range(2):
+            keys = w.k[w.seen(i, new), 0]
+            score = keys @ q[i, h] * dim ** -0.5
+            top = score.topk(2)
+            off = 2.0 ** -16 * (keys.abs() @ q[i, h].abs()).max() * dim ** -0.5
+            if top.values[0] - top.values[1] > 40 + 2 * off:
+                want = w.v[top.indices[0], 0]
+                assert ((got[i, h] - want).abs() <= 2.0 ** -8 * want.abs()).all(), (i, h)
+                checked += 1
+    assert checked > 0
+
+
+@pytest.mark.parametrize("new,copies", [FEW, MANY])
+@pytest.mark.parametrize("size", [2.0 ** 9, 2.0 ** 13, 2.0 ** 15, 2.0 ** 16, 2.0 ** 25])
+def test_equal_scores_of_any_size_weigh_the_same(torch, KV, size, new, copies):
+    """Two equal keys above all others, whatever their score is rounded to: the mean of their values."""
+    k, q = normal(torch, 4, 300, 1, 128), normal(torch, 5, 1, 1, 128)
+    k[70] = k[71] = q[0] * 4
+    w = Sequence(torch, KV, k * size, normal(torch, 6, 300, 1, 128))
+    got, _ = w.attend((q * size).expand(new, 2, 128), copies)
+    want = w.v[70:72, 0].mean(0)
+    assert ((got[[0, new - 1]] - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -16 * w.v[70:72, 0].abs().sum(0)).all()
+
+
+@pytest.mark.parametrize("new,copies", [FEW, MANY])
+def test_a_score_that_passes_fp32_is_not_left_out(torch, KV, new, copies):
+    """q and k finite, their product not: NaN, not the answer without that key."""
+    k, v = normal(torch, 7, 300, 1, 64), normal(torch, 8, 300, 1, 64)
+    k[50] = 1e25
+    w = Sequence(torch, KV, k, v)
+    got, _ = w.attend(torch.full((new, 1, 64), 1e25), copies)
+    assert bool(torch.isnan(got[[0, new - 1]]).all())
