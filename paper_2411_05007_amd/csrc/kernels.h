@@ -249,7 +249,7 @@ struct KvAttentionParams {
     int row_tiles;           // few-row kernel: tiles of 16 rows a sequence and head may need
     int row_cap;             // few-row kernel: rows that a tile can have
     int chunk_blocks, chunks;      // few-row kernel: the keys are cut into chunks of chunk_blocks blocks (the last takes the rest)
-    float *partial;          // chunks > 1: fp32 [sequence][row tile][head][chunk]([row_cap][dim] sums, [row_cap][2] maximum and sum of weights)
+    float *partial;          // chunks > 1: fp32 [sequence][row tile][head][chunk]([row_cap][dim] weighted means of values, [row_cap][2] maximum and sum of weights)
     float *part_ml;          // parts > 1: fp32 [part][row][2] maximum and sum of weights, rows as in out; partial [part][row][dim]
     unsigned long long *arrived;      // chunks > 1: [sequence][row tile][head][chunk]
 };

@@ -35,11 +35,11 @@ constexpr int WAVES = 4;
 template <int D>
 struct Block { uint4 k[2][D / 64]; uint4 v[D / 32]; };      // 32 tokens of a head, as a lane holds them
 
-// floats of a row in LDS, and the bytes of a workgroup's LDS: first the queries as operands in fp32 and maxima per wavefront, then [wave][row][row_floats], then maximum and sum [wave][16][2], then the reference exponents
+// floats of a row in LDS, and the bytes of a workgroup's LDS: first the queries as operands in fp32 and maxima per wavefront, then [wave][row][row_floats] and maximum and sum
+// [wave][16][2], or, where parts meet, weights [chunk][row] and 16 bytes a thread
 constexpr int row_floats(int D) { return D + 4; }
-// or, where parts meet: weights [chunk][row], a factor per row, 16 bytes a thread
 constexpr int rows_lds_bytes(int D, int waves, int cap, int chunks) {
-    const int loop = (waves * cap * row_floats(D) + waves * 32 + waves) * 4, queries = (D / 32 * 512 + waves * 64) * 4, parts = chunks > 1 ? (chunks * cap + cap + 8) * 4 + waves * 64 * 16 : 0;
+    const int loop = (waves * cap * row_floats(D) + waves * 32) * 4, queries = (D / 32 * 512 + waves * 64) * 4, parts = chunks > 1 ? (chunks * cap + 4) * 4 + waves * 64 * 16 : 0;
     return loop > parts ? loop > queries ? loop : queries : parts > queries ? parts : queries;
 }
 constexpr int kAgent = 16;      // cache policy of a buffer access that all XCDs see
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     constexpr int kRow = row_floats(D);
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const int cap = p.row_cap;                   // rows that a tile can have
-    float *sums = lds, *ml = lds + WAVES * cap * kRow, *refs = ml + WAVES * 32;
+    float *sums = lds, *ml = lds + WAVES * cap * kRow;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, q4 = lane >> 4;
     const int head = blockIdx.y, b = blockIdx.z / p.row_tiles, tile = blockIdx.z % p.row_tiles;
@@ -244,62 +244,51 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
         load(odd, 1);
     }
 
-    // ---- the wavefronts' sums meet ----
+    // ---- the wavefronts meet: as weighted means of values, which pass no range that the values themselves keep (their sums may) ----
     __syncthreads();      // (the queries lay there)
     l = kv_sum32(kv_sum16(l));
     if (q4 == 0) {
         ml[(wave * 16 + l16) * 2] = m;
         ml[(wave * 16 + l16) * 2 + 1] = l;
     }
-    if (lane == 0) refs[wave] = (float)ref;
-    __syncthreads();
-    {
-        float top = kNone, most = 0.f;
+    if (l16 < cap) {
+        const float inv = kv_inverse(l), f = kv_pow2(ref - 127);
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            top = fmaxf(top, ml[(w * 16 + l16) * 2]);
-            most = fmaxf(most, refs[w]);
-        }
-        const float f = __builtin_amdgcn_exp2f(m - top) * kv_pow2(ref - (int)most);
-        if (l16 < cap)
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) *reinterpret_cast<kv_floatx4 *>(sums + (wave * cap + l16) * kRow + 16 * d + 4 * q4) = o[d] * f;
+        for (int d = 0; d < D / 16; ++d) *reinterpret_cast<kv_floatx4 *>(sums + (wave * cap + l16) * kRow + 16 * d + 4 * q4) = o[d] * inv * f;
     }
     __syncthreads();
     // pieces of four channels of a row
     const long long part = ((long long)blockIdx.z * p.cache.heads + head) * p.chunks;      // of this row tile's parts
     const int live_rows = rows - tile * 16 < 16 ? rows - tile * 16 : 16, pieces = live_rows * (D / 4);
-    const size_t part_floats = (size_t)cap * (D + 2);      // [cap][D] sums, [cap][2] maximum and sum of weights
+    const size_t part_floats = (size_t)cap * (D + 2);      // [cap][D] weighted means, [cap][2] maximum and sum of weights
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.partial + part * part_floats, (size_t)nchunks * part_floats * 4);
-    auto store = [&](int row, int d, kv_floatx4 x, float inv) {
+    auto store = [&](int row, int d, kv_floatx4 x) {
         const int rr = tile * 16 + row;
         uint16_t *dst = p.out + ((size_t)(t0 + rr / p.group) * p.q_heads + head * p.group + rr % p.group) * D + d;
-        const kv_bf16x2 lo = {(__bf16)(x[0] * inv), (__bf16)(x[1] * inv)}, hi = {(__bf16)(x[2] * inv), (__bf16)(x[3] * inv)};
+        const kv_bf16x2 lo = {(__bf16)x[0], (__bf16)x[1]}, hi = {(__bf16)x[2], (__bf16)x[3]};
         *reinterpret_cast<uint2 *>(dst) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
     };
-    auto inverse = [](float sum) { return sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum; };      // (no key seen: zeros)
     for (int i = threadIdx.x; i < pieces; i += WAVES * 64) {
         const int row = i / (D / 4), d = i % (D / 4) * 4;
-        float top = kNone, most = 0.f;
+        float top = kNone;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[(w * 16 + row) * 2]);
+        float weight[WAVES], sum = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            top = fmaxf(top, ml[(w * 16 + row) * 2]);
-            most = fmaxf(most, refs[w]);
+            weight[w] = ml[(w * 16 + row) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(w * 16 + row) * 2] - top);
+            sum += weight[w];
         }
+        const float inv = kv_inverse(sum);
         kv_floatx4 x = {};
-        float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            x += *reinterpret_cast<const kv_floatx4 *>(sums + (w * cap + row) * kRow + d);
-            sum += ml[(w * 16 + row) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(w * 16 + row) * 2] - top);
-        }
-        x *= kv_pow2((int)most - 127);
+        for (int w = 0; w < WAVES; ++w) x += *reinterpret_cast<const kv_floatx4 *>(sums + (w * cap + row) * kRow + d) * (weight[w] * inv);
         if (nchunks > 1) {      // past the L2 of this XCD: the workgroup that adds the parts may run on another
             const int at = (int)(chunk * part_floats * 4);
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(kv_u32x4, x), rs, at + (row * D + d) * 4, 0, kAgent);
             if (d == 0) __builtin_amdgcn_raw_buffer_store_b64(kv_u32x2{__float_as_uint(top), __float_as_uint(sum)}, rs, at + (cap * D + row * 2) * 4, 0, kAgent);
         } else {
-            store(row, d, x, inverse(sum));
+            store(row, d, x);
         }
     }
     if (nchunks == 1) return;
@@ -319,9 +308,8 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     }
     __syncthreads();
     if (missing) return;
-    // weights of the parts, [chunk][row], then 1 / their sum per row; thread groups add every so many parts, and the groups meet in LDS
-    float *weight = lds, *inv_of = weight + nchunks * cap, *meet = inv_of + ((cap + 3) & ~3);
-    meet = lds + (((meet - lds) + 3) & ~3);
+    // weights of the parts, [chunk][row], of sum 1 in a row; thread groups add every so many parts, and the groups meet in LDS
+    float *weight = lds, *meet = lds + ((nchunks * cap + 3) & ~3);
     for (int row = wave; row < live_rows; row += WAVES) {
         float mx = kNone, part_m[kKvMostChunks / 64], part_l[kKvMostChunks / 64];
 #pragma unroll
@@ -338,14 +326,15 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < kKvMostChunks / 64; ++k) {
-            const int c = lane + 64 * k;
-            const float f = __builtin_amdgcn_exp2f(part_m[k] - mx);
-            sum += part_l[k] * f;
-            if (c < nchunks) weight[c * cap + row] = f;
+            part_l[k] *= __builtin_amdgcn_exp2f(part_m[k] - mx);
+            sum += part_l[k];
         }
 #pragma unroll
         for (int s = 1; s < 64; s *= 2) sum += __shfl_xor(sum, s);
-        if (lane == 0) inv_of[row] = inverse(sum);
+        const float inv = kv_inverse(sum);
+#pragma unroll
+        for (int k = 0; k < kKvMostChunks / 64; ++k)
+            if (lane + 64 * k < nchunks) weight[(lane + 64 * k) * cap + row] = part_l[k] * inv;
     }
     __syncthreads();
     const int groups = pieces < WAVES * 64 ? WAVES * 64 / pieces : 1, mine = threadIdx.x / pieces;
@@ -373,10 +362,10 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
             __syncthreads();
             if (mine == 0) {
                 for (int g = 1; g < groups; ++g) x += *reinterpret_cast<const kv_floatx4 *>(meet + (g * pieces + threadIdx.x) * 4);
-                store(row, d, x, inv_of[row]);
+                store(row, d, x);
             }
         } else if (works) {
-            store(row, d, x, inv_of[row]);
+            store(row, d, x);
         }
     }
     // (every workgroup of the row tile has made its mark; two that both found all marks store the same results)

@@ -10,7 +10,7 @@
 // between lane halves away.  Statistics in fp32; P is exp2(t - m + 8) in f16, at most 2^14 before the maximum is renewed, so weights down to 2^-22 of the
 // largest keep eleven bits; Q in f16, scaled by a power of two per row, for the same eleven bits.
 // The scores of a tile are made beside the weights of the one before, codes are requested two and three tiles ahead, pages and scale bytes 32 tiles ahead; one barrier a tile.
-// Few row tiles on many keys take parts of the keys, which kv_meet_kernel adds.  A wavefront whose rows are past the sequence's only carries codes.
+// Few row tiles on many keys take parts of the keys, which kv_meet_kernel joins.  A wavefront whose rows are past the sequence's only carries codes.
 // Bound: matrix cores and vector ALU, which overlap little, at the chip's power limit (2.05 of 2.4 GHz).  8192 tokens, 32 query heads on 8, on 16384 keys 1530 us, 1.08 PFLOP/s
 // (a library product of 8192 cubed in f16 reaches 1.215): matrix cores busy 52 % of the time, vector ALU 55 %; 4608 tokens of 24 heads, all with all, 279 us, 49 and 54 %, and 432
 // tiles are two rounds of 256 CUs; six ragged chunks of up to 2111 tokens 355 us, 43 and 57 %.  What a workgroup of 128 rows costs beside its tiles (1.05 us each): scan over
@@ -464,11 +464,11 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     // ---- the way out: 32 rows x kOut channels at a time through the wavefront's part of LDS, so that a store writes whole rows ----
     const float sum = kv_sum32(l);
     const bool parts = p.parts > 1;
-    const float f = parts ? kv_pow2(ref - 127) : (sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum) * kv_pow2(ref - 127);      // (no key seen: zeros)
+    const float inv = kv_inverse(sum), f = kv_pow2(ref - 127);      // (one after the other: their product may leave fp32's range where the mean does not)
     const size_t out_rows = (size_t)p.batch.total * p.q_heads;
     auto out_row = [&](int r) { return (size_t)(t0 + r / p.group) * p.q_heads + head * p.group + r % p.group; };
     const int r_lane = row0 + wave * 32 + l32;
-    if (parts) {      // [part][row][D] and [part][row][2], to be added by kv_meet_kernel
+    if (parts) {      // weighted means [part][row][D] and [part][row][2], to be joined by kv_meet_kernel
         if (h32 == 0 && r_lane < rows) *reinterpret_cast<float2 *>(p.part_ml + (part * out_rows + out_row(r_lane)) * 2) = make_float2(m, sum);
         if (tiles_k == 0) return;
     }
@@ -482,7 +482,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         for (int a = a0; a < a0 + 2; ++a)
 #pragma unroll
             for (int v = 0; v < 16; v += 4)
-                *reinterpret_cast<float4 *>(my_rows + l32 * kOutRow + (32 * (a - a0) + 2 * v + 4 * h32) * 4) = make_float4(o[a][v] * f, o[a][v + 1] * f, o[a][v + 2] * f, o[a][v + 3] * f);
+                *reinterpret_cast<float4 *>(my_rows + l32 * kOutRow + (32 * (a - a0) + 2 * v + 4 * h32) * 4) = make_float4(o[a][v] * inv * f, o[a][v + 1] * inv * f, o[a][v + 2] * inv * f, o[a][v + 3] * inv * f);
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {      // eight channels a lane, eight rows a time
@@ -503,7 +503,8 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     }
 }
 
-// Adds the parts of every row in order: weights exp2(m_part - max), then one division.  A thread has four channels of a row.
+// Joins the parts of every row in order: each is a weighted mean of values, and they are weighted with their share of the weights, so nothing passes a range that
+// the values keep.  A thread has four channels of a row.
 template <int D>
 __global__ __launch_bounds__(256) void kv_meet_kernel(KvAttentionParams p) {
     constexpr int kRows = 256 / (D / 4);      // rows of a workgroup
@@ -515,19 +516,23 @@ __global__ __launch_bounds__(256) void kv_meet_kernel(KvAttentionParams p) {
     last = last > p.batch.total ? p.batch.total : last;
     const long long token = (long long)(row / p.q_heads);
     if (row >= rows || token < first || token >= last) return;
-    float most = kNone;
-    for (int i = 0; i < p.parts; ++i) most = fmaxf(most, p.part_ml[((size_t)i * rows + row) * 2]);
-    kv_floatx4 x = {};
-    float sum = 0.f;
-    for (int i = 0; i < p.parts; ++i) {
-        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + ((size_t)i * rows + row) * 2);
-        if (ml.y == 0.f) continue;            // (a part that saw no key holds no sums)
-        const float f = __builtin_amdgcn_exp2f(ml.x - most);
-        x += *reinterpret_cast<const kv_floatx4 *>(p.partial + ((size_t)i * rows + row) * D + d) * f;
-        sum += ml.y * f;
+    float2 ml[kKvMostParts];
+    float most = kNone, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kKvMostParts; ++i) ml[i] = i < p.parts ? *reinterpret_cast<const float2 *>(p.part_ml + ((size_t)i * rows + row) * 2) : make_float2(kNone, 0.f);
+#pragma unroll
+    for (int i = 0; i < kKvMostParts; ++i) most = fmaxf(most, ml[i].x);
+#pragma unroll
+    for (int i = 0; i < kKvMostParts; ++i) {
+        ml[i].y *= __builtin_amdgcn_exp2f(ml[i].x - most);
+        sum += ml[i].y;
     }
-    const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
-    const kv_bf16x2 lo = {(__bf16)(x[0] * inv), (__bf16)(x[1] * inv)}, hi = {(__bf16)(x[2] * inv), (__bf16)(x[3] * inv)};
+    const float inv = kv_inverse(sum);
+    kv_floatx4 x = {};
+#pragma unroll
+    for (int i = 0; i < kKvMostParts; ++i)
+        if (ml[i].y != 0.f) x += *reinterpret_cast<const kv_floatx4 *>(p.partial + ((size_t)i * rows + row) * D + d) * (ml[i].y * inv);      // (a part that saw no key holds no mean)
+    const kv_bf16x2 lo = {(__bf16)x[0], (__bf16)x[1]}, hi = {(__bf16)x[2], (__bf16)x[3]};
     *reinterpret_cast<uint2 *>(p.out + row * D + d) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
 }
 

@@ -769,7 +769,7 @@ inline Workspace workspace_layout(int M, int K, int N, int rank, int ksplit_over
 
 // ---- attention over the paged 8-bit cache: which kernel, and how the keys are cut --------------------------------------------------------
 constexpr unsigned long long kKvArrived = 0x4b56535644514152ull;      // as kActArrived: what a workgroup leaves in its arrival word
-constexpr int kKvMostChunks = 256;
+constexpr int kKvMostChunks = 256, kKvMostParts = 16;
 struct KvPlan {
     bool few, many;                                    // the kernel of sixteen rows a workgroup (kv_rows_kernel.hip), the one of 128 or 256 (kv_tile_kernel.hip), or each for its sequences
     int row_tiles, row_cap, chunk_blocks, chunks;      // few
@@ -799,7 +799,7 @@ inline int kv_chunk_blocks(long long wgs, int blocks) {
 inline int kv_parts(long long wgs, long long slots, long long keys) {
     long long n = wgs > 0 ? slots / wgs : 1;
     n = n > keys / 512 ? keys / 512 : n;
-    return n < 1 ? 1 : n > 16 ? 16 : (int)n;
+    return n < 1 ? 1 : n > kKvMostParts ? kKvMostParts : (int)n;
 }
 // The kernel by what each is estimated to cost, in ns.  Few: 10 us, and 0.75 ns for a row tile and block of all CUs (head size 128).  Many: 15 us, 12 more where parts meet, and
 // 2.2 us for each 64 keys of a round of workgroups.  Measured, us, few | many: 64 sequences of 64 rows (eight key heads) on 4000 keys 169 | 150, of 128

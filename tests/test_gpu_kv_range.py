@@ -122,3 +122,25 @@ def test_a_score_that_passes_fp32_is_not_left_out(torch, KV, new, copies):
     w = Sequence(torch, KV, k, v)
     got, _ = w.attend(torch.full((new, 1, 64), 1e25), copies)
     assert bool(torch.isnan(got[[0, new - 1]]).all())
+
+
+def close(w, got, q, i, h, **kw):
+    """Row i and head h within what its arithmetic allows: queries without a rotation are exact in f16, fp32 scores are off by 2^-16 of their products' magnitudes, weights are
+    rounded to 11 bits and summed in fp32, the output to 8; what is below 2^-33 of the largest weight may be left out, of the values that the row sees."""
+    want, size = w.want(q, i, h, **kw)
+    keys, kh = w.seen(i, q.shape[0], kw.get("causal", True), kw.get("window", 0)), h // (q.shape[1] // w.heads)
+    scale = w.D ** -0.5 if kw.get("scale") is None else abs(kw["scale"])
+    d = 2.0 ** -16 * scale * float((w.k[keys, kh].abs() @ q[i, h].abs()).max())
+    tol = 2.0 ** -8 * want.abs() + (np.expm1(2 * d) + 2.0 ** -10 + 2.0 ** -14) * size + w.k[keys].shape[0] * 2.0 ** -33 * w.v[keys, kh].abs().max()
+    off = (got[i, h] - want).abs() - tol
+    assert bool((off <= 0).all()), (i, h, float(off.max()), got[i, h, :4], want[:4])
+
+
+@pytest.mark.parametrize("new,copies,L", [(*FEW, 700), (*FEW, 9000), (3, 40, 300), (*MANY, 700), (300, 1, 9000)])      # whole keys and cut ones, in both kernels
+@pytest.mark.parametrize("dim,size", [(128, 2.0 ** 126), (64, 1e33), (256, 1e35), (128, 1e-33), (64, 2.0 ** -116), (128, 2.0 ** -120)])
+def test_sums_of_values_keep_the_values_range(torch, KV, dim, size, new, copies, L):
+    """Values about as large, or as small, as 16-bit numbers are: their mean is a number like them, though their sum need not be."""
+    w = Sequence(torch, KV, normal(torch, 9, L, 1, dim), (normal(torch, 10, L, 1, dim).clamp(-4, 4) * 0.1 + 1) * size)
+    got, q = w.attend(normal(torch, 11, new, 4, dim), copies)
+    for i in {0, 1, new - 1} & set(range(new)):
+        close(w, got, q, i, i % 4)
