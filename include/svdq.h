@@ -440,8 +440,10 @@ int svdq_kv_append(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, c
  * Attention of the batch's new tokens over the cache, which holds them already:
  *   O = softmax(scale Q' K^T) V,  Q' = Q rotated;  query head h reads key head h / (q_heads / kv_heads).
  *   causal: position p sees positions 0 .. p, with window > 0 only the last `window` of them; otherwise all kv_len.
- * Scores, softmax statistics and sums are fp32; rotated queries and the weights exp(s - max) are rounded to f16 (11 bits, scaled
- * so that none is lost to its range), codes times scales are exact.  A row that sees no key is zero.
+ * Scores, softmax statistics and sums are fp32 (a score past its range makes its row NaN).  Rotated queries are rounded to f16, scaled by a power of two per row: 11 bits,
+ * fewer for channels below 2^-28 of the row's largest, none below 2^-39.  So are the weights exp(s - max): 11 bits, fewer below 2^-22 of the largest, none below 2^-33.
+ * Codes times scales are exact, whatever a row does not see: where the scales of values are more than 2^15 apart, every 32 keys count by themselves, and "the largest" weight
+ * is the largest among them.  A row that sees no key is zero.
  *   out: device bf16 [new_tokens][q_heads][head_dim], 16-byte aligned
  *   workspace: device, 256-byte aligned, >= svdq_kv_attention_workspace_bytes(); needs no initial contents.  Two calls that share one must be ordered on one stream.
  *   Its size: up to 34 MB for the parts of chunks, and for single tokens the fp32 sums of up to 16 rows for each sequence, key head and 4096 to 8192 keys.

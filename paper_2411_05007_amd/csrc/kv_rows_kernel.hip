@@ -6,7 +6,8 @@
 // chunks, a workgroup of four wavefronts has one chunk of one head, a wavefront takes every fourth block of 32 tokens: S^T = K Q^T by
 // v_mfma_f32_16x16x32_f16 with the codes of the keys as exact f16 numbers (rows of the operand: tokens, in an order that makes the accumulators of
 // two such products the operand of the next), the block's scale in one factor per row; running maximum and sum per row in fp32; P^T in f16;
-// O^T += V^T P^T with the values as code * 2^(byte - reference), exact, the reference exponent the largest seen.  P is scaled by 2^8 (and may reach 2^14
+// O^T += V^T P^T with the values as code * 2^(byte - reference), the reference exponent the largest so far, which is exact while the wavefront's bytes are at most
+// 15 apart (kv_common.h has the other way).  P is scaled by 2^8 (and may reach 2^14
 // before the maximum is renewed), so that f16 keeps eleven bits of weights down to 2^-22 of the largest; f16 for Q, scaled by a power of two per
 // row, for the same eleven bits.
 // Loads: the pages and scale bytes of a wavefront's next 64 blocks are looked up at once, one in a lane; the codes of two blocks are in flight (16 KB a
@@ -167,8 +168,9 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     float m = kNone, l = 0.f;
     int ref = 0;                                 // byte of the reference scale of the values in o
 
-    auto step = [&](Block<D> &cur, int i) {
-        const int blk = base + WAVES * i, kb = __builtin_amdgcn_readlane(kb_l, i), vb = __builtin_amdgcn_readlane(vb_l, i);
+    // exponents t of block i's weights, -inf where the row does not see the token; values of tokens that do not exist are cleared
+    auto scores = [&](Block<D> &cur, int i, float (&t)[8]) {
+        const int blk = base + WAVES * i, kb = __builtin_amdgcn_readlane(kb_l, i);
         const bool named = __builtin_amdgcn_readlane(page_l, i) >= 0;
         kv_floatx4 s[2] = {};
 #pragma unroll
@@ -180,7 +182,6 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
             }
         // the lane's eight tokens are those of slot q4
         const float f = to_t * kv_pow2(kb - 127);
-        float t[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) t[j] = s[j / 4][j % 4] * f;
         if (!named || blk * kKvBlock < all_lo || blk * kKvBlock + kKvBlock > all_hi) {
@@ -198,10 +199,18 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
                 cur.v[a].x &= live[0]; cur.v[a].y &= live[1]; cur.v[a].z &= live[0]; cur.v[a].w &= live[1];
             }
         }
+    };
+    auto largest_of = [&](const float (&t)[8]) {      // of the row
         float top = t[0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) top = fmaxf(top, t[j]);
-        top = kv_max32(kv_max16(top));
+        return kv_max32(kv_max16(top));
+    };
+    auto step = [&](Block<D> &cur, int i) {
+        const int vb = __builtin_amdgcn_readlane(vb_l, i);
+        float t[8];
+        scores(cur, i, t);
+        const float top = largest_of(t);
         const int ref_new = vb > ref ? vb : ref;
         if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0ull || ref_new != ref) {
             const float m_new = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(m - m_new);
@@ -226,7 +235,11 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
             o[2 * a + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(cur.v[a].z, cur.v[a].w, vf), pf, o[2 * a + 1], 0, 0, 0);
         }
     };
+    KvSpread spread;
+    bool wide = false;      // the values' scales are too far apart for one reference
     for (;;) {
+        wide = spread.add(page_l >= 0 ? vb_l : 0);
+        if (wide) break;
         for (int i = 0; i < here; i += 2) {
             step(even, i);
             load(even, i + 2);
@@ -243,6 +256,53 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
         load(even, 0);
         load(odd, 1);
     }
+    int row_ref = ref;
+    if (__builtin_expect(wide, 0)) {      // from the start, a block at a time
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[d] = kv_floatx4{};
+        m = kNone;
+        l = 0.f;
+        row_ref = 0;
+        base = c0 + wave;
+        left = (c1 - base + WAVES - 1) / WAVES;
+        for (;;) {
+            look_up();
+            look_up_bytes();
+            for (int i = 0; i < here; ++i) {
+                load(even, i);
+                float t[8];
+                scores(even, i, t);
+                const float top = largest_of(t), from = top > -__builtin_inff() ? top : 0.f;
+                kv_f16x8 pf;
+                float sum = 0.f, largest = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(t[j] - from + kShift);
+                    sum += e;
+                    pf[j] = (_Float16)e;
+                }
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) largest = fmaxf(largest, __builtin_fabsf(o[d][j]));
+                const KvJoin join = kv_join(m, row_ref, top, __builtin_amdgcn_readlane(vb_l, i), kv_max32(kv_max16(largest)));
+                l = l * join.keep_l + sum * join.add_l;
+#pragma unroll
+                for (int a = 0; a < D / 32; ++a) {
+                    const kv_floatx4 x = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(even.v[a].x, even.v[a].y, 1.f), pf, kv_floatx4{}, 0, 0, 0);
+                    const kv_floatx4 y = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(even.v[a].z, even.v[a].w, 1.f), pf, kv_floatx4{}, 0, 0, 0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        o[2 * a][j] = __builtin_amdgcn_ldexpf(o[2 * a][j] * join.keep, join.keep_e) + __builtin_amdgcn_ldexpf(x[j] * join.add, join.add_e);
+                        o[2 * a + 1][j] = __builtin_amdgcn_ldexpf(o[2 * a + 1][j] * join.keep, join.keep_e) + __builtin_amdgcn_ldexpf(y[j] * join.add, join.add_e);
+                    }
+                }
+            }
+            left -= here;
+            if (left <= 0) break;
+            base += WAVES * 64;
+        }
+    }
 
     // ---- the wavefronts meet: as weighted means of values, which pass no range that the values themselves keep (their sums may) ----
     __syncthreads();      // (the queries lay there)
@@ -252,9 +312,14 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
         ml[(wave * 16 + l16) * 2 + 1] = l;
     }
     if (l16 < cap) {
-        const float inv = kv_inverse(l), f = kv_pow2(ref - 127);
+        const float inv = kv_inverse(l);
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) *reinterpret_cast<kv_floatx4 *>(sums + (wave * cap + l16) * kRow + 16 * d + 4 * q4) = o[d] * inv * f;
+        for (int d = 0; d < D / 16; ++d) {
+            kv_floatx4 x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_ldexpf(o[d][j] * inv, row_ref - 127);
+            *reinterpret_cast<kv_floatx4 *>(sums + (wave * cap + l16) * kRow + 16 * d + 4 * q4) = x;
+        }
     }
     __syncthreads();
     // pieces of four channels of a row

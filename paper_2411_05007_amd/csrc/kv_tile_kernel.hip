@@ -5,7 +5,7 @@
 // The rows of a sequence and key head are its new tokens times the query heads that share the head, so a tile of keys serves the whole group.  A
 // workgroup has 128 rows (four wavefronts, two workgroups on a CU) or 256 (eight, one; head size 128, long even batches), 32 to a wavefront; keys and values go by
 // in tiles of 64 tokens, read once per workgroup as codes, converted to f16 on the way into LDS (exact: codes of the keys, code * 2^(byte - reference) of the values, the
-// reference exponent the largest seen) and laid out as operands, so that an operand read is 64 lanes x 16 bytes in a row.  S^T = K Q^T by
+// reference exponent the largest so far, while the bytes are at most 15 apart: kv_common.h has the other way) and laid out as operands, so that an operand read is 64 lanes x 16 bytes in a row.  S^T = K Q^T by
 // v_mfma_f32_32x32x16_f16: a lane has one row of queries, its accumulators are the operand of O^T = V^T P^T as they stand, and maximum and sum of a row are one exchange
 // between lane halves away.  Statistics in fp32; P is exp2(t - m + 8) in f16, at most 2^14 before the maximum is renewed, so weights down to 2^-22 of the
 // largest keep eleven bits; Q in f16, scaled by a power of two per row, for the same eleven bits.
@@ -72,9 +72,11 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
 
     // ---- the way of the codes: pages and scale bytes of 64 blocks (32 tiles) at a time, one in a lane; codes by way of registers ----
     const int32_t *table = p.batch.table + (size_t)b * p.batch.table_width;
-    const int bs = p.cache.page_shift - 5, blk0 = key0 >> 5, blk1 = (wg_hi + 31) >> 5;
+    const int bs = p.cache.page_shift - 5, blk0 = key0 >> 5, blk_z = (wg_hi + 31) >> 5, blk1 = blk_z < blk0 + 2 * tiles_k ? blk_z : blk0 + 2 * tiles_k;
     // (a unit is a block of a head, 2 KB of codes at least: 32 bits count them)
     int unit_l = -1, kb_l = 0, vb_l = 0, unit_a = -1, kb_a = 0, vb_a = 0;      // of the window in use, and of the one after it; -1: no such block
+    KvSpread spread;
+    bool wide = false;      // the values' scales are too far apart for one reference (the same in all wavefronts)
     auto look_up_pages = [&](int t) {      // t a multiple of 32
         const int blk = blk0 + 2 * t + lane;
         unit_a = blk < blk1 ? table[blk >> bs] : -1;
@@ -90,6 +92,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         unit_l = unit_a;
         kb_l = kb_a;
         vb_l = unit_a == -1 ? 0 : vb_a;
+        wide = wide || spread.add(vb_l);
     };
     // what is known of a tile: its blocks and their scale bytes
     struct Facts { int unit[2], kb[2], vb[2]; };
@@ -228,7 +231,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     uint4 kw[2][N], vw[2][N];      // codes on their way: of keys and values of even and odd tiles
     next_window();
     Facts f0 = facts_of(0), f1 = facts_of(1), f2 = facts_of(2), f3 = facts_of(3), f4 = facts_of(4);      // of tiles t .. t + 4
-    if (tiles_k > 0) {
+    if (tiles_k > 0 && !wide) {
         request(kw[0], p.cache.k, f0);
         request(vw[0], p.cache.v, f0);
         request(kw[1], p.cache.k, f1);
@@ -336,7 +339,9 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         f3 = f4;
         f4 = facts_of(far);
     };
-    if (tiles_k > 0) {
+    // (a window of pages that turns out too wide ends both loops below at the same step: it is one of tiles that are still to come, four at least)
+    const bool ordinary = tiles_k > 0 && !wide;
+    if (ordinary) {
         ref = refer(f0);
         clear_unnamed(vw[0], f0);
 #pragma unroll
@@ -351,7 +356,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         request(kw[1], p.cache.k, f3);
         kv_lds_barrier();
     }
-    if (tiles_k > 0 && idle) {      // a wavefront's part of the steps but for its products
+    if (ordinary && idle) {      // a wavefront's part of the steps but for its products
         kv_lds_barrier();
         auto carry = [&](uint4 (&kn)[N], uint4 (&vn)[N], int t) {
             ref = refer(f1) > ref ? refer(f1) : ref;
@@ -366,11 +371,11 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
             kv_lds_barrier();
             advance(t + 5);
         };
-        for (int t = 0; t + 1 < tiles_k; t += 2) {
+        for (int t = 0; t + 1 < tiles_k && !wide; t += 2) {
             carry(kw[0], vw[1], t);
             if (t + 2 < tiles_k) carry(kw[1], vw[0], t + 1);
         }
-    } else if (tiles_k > 0) {
+    } else if (ordinary) {
         Scores even, odd;
         float top[2];
         even[0] = even[1] = kv_floatx16{};
@@ -439,32 +444,91 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
             advance(t + 5);
         };
         int t = 0;
-        for (; t + 4 <= tiles_k; t += 2) {      // (the last tile's values may be partial: step tiles_k - 2)
+        for (; t + 4 <= tiles_k && !wide; t += 2) {      // (the last tile's values may be partial: step tiles_k - 2)
             step(even, odd, kw[0], vw[1], t, std::false_type{});
             step(odd, even, kw[1], vw[0], t + 1, std::false_type{});
         }
-        // one to three tiles are left, the first one's scores in `even`
-        if (t + 1 < tiles_k) {
-            step(even, odd, kw[0], vw[1], t, std::true_type{});
-            ++t;
+        if (!wide) {      // one to three tiles are left, the first one's scores in `even`
             if (t + 1 < tiles_k) {
-                step(odd, even, kw[1], vw[0], t, std::true_type{});
+                step(even, odd, kw[0], vw[1], t, std::true_type{});
                 ++t;
-            } else {
-                even[0] = odd[0];
-                even[1] = odd[1];
+                if (t + 1 < tiles_k) {
+                    step(odd, even, kw[1], vw[0], t, std::true_type{});
+                    ++t;
+                } else {
+                    even[0] = odd[0];
+                    even[1] = odd[1];
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q) weight_pair(even, q);
+#pragma unroll
+            for (int k = 0; k < 4 * A; ++k) add_values(value_operand(vt(t), k), k);
+        }
+    }
+    int row_ref = ref;
+    if (__builtin_expect(wide && !idle, 0)) {      // from the start, a block at a time, each wavefront by itself
+#pragma unroll
+        for (int a = 0; a < A; ++a) o[a] = kv_floatx16{};
+        m = kNone;
+        l = 0.f;
+        row_ref = 0;
+        const int pos = pos_of(row0 + wave * 32 + l32), seen_hi = hi_of(pos) < len ? hi_of(pos) : len, seen_lo = lo_of(pos);
+        for (int blk = blk0; blk < blk1; ++blk) {
+            const long long unit = kv_unit(p.cache, p.batch.table, p.batch.table_width, b, head, blk);
+            if (unit < 0) continue;
+            const uint8_t *k = p.cache.k + (size_t)unit * (32 * D) + l32 * D + 8 * h32, *v = p.cache.v + (size_t)unit * (32 * D) + (l32 % 16 * 4 + h32) * 16 + l32 / 16 * 8;
+            kv_floatx16 s = {};
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const uint2 w = *reinterpret_cast<const uint2 *>(k + 16 * c);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv_f16_of(w.x, w.y, 1.f), qf[c], s, 0, 0, 0);
+            }
+            const float f = to_t * kv_pow2((int)p.cache.ks[unit] - 127);
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int at = blk * kKvBlock + 8 * (i >> 2) + 4 * h32 + (i & 3);
+                s[i] = at >= seen_lo && at < seen_hi ? s[i] * f : -__builtin_inff();
+                top = fmaxf(top, s[i]);
+            }
+            top = kv_max32(top);
+            const float from = top > -__builtin_inff() ? top : 0.f;
+            float sum = 0.f, largest_o = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const _Float16 e = (_Float16)__builtin_amdgcn_exp2f(s[i] - from + kShift);
+                sum += (float)e;
+                pf[i / 8][i % 8] = e;
+            }
+#pragma unroll
+            for (int a = 0; a < A; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) largest_o = fmaxf(largest_o, __builtin_fabsf(o[a][i]));
+            const KvJoin join = kv_join(m, row_ref, top, (int)p.cache.vs[unit], kv_max32(largest_o));
+            l = l * join.keep_l + sum * join.add_l;
+#pragma unroll
+            for (int a = 0; a < A; ++a) {
+                kv_floatx16 x = {};
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {      // the lane's slot is 2 g + h32
+                    uint2 w = *reinterpret_cast<const uint2 *>(v + a * 1024 + g * 32);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (blk * kKvBlock + kv_slot_token(2 * g + h32) + (j & 3) + 8 * (j >> 2) >= len) (j < 4 ? w.x : w.y) &= ~(0xffu << (8 * (j & 3)));
+                    x = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv_f16_of(w.x, w.y, 1.f), pf[g], x, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[a][i] = __builtin_amdgcn_ldexpf(o[a][i] * join.keep, join.keep_e) + __builtin_amdgcn_ldexpf(x[i] * join.add, join.add_e);
             }
         }
-#pragma unroll
-        for (int q = 0; q < 16; ++q) weight_pair(even, q);
-#pragma unroll
-        for (int k = 0; k < 4 * A; ++k) add_values(value_operand(vt(t), k), k);
     }
 
     // ---- the way out: 32 rows x kOut channels at a time through the wavefront's part of LDS, so that a store writes whole rows ----
     const float sum = kv_sum32(l);
     const bool parts = p.parts > 1;
-    const float inv = kv_inverse(sum), f = kv_pow2(ref - 127);      // (one after the other: their product may leave fp32's range where the mean does not)
+    const float inv = kv_inverse(sum);
+    const auto mean = [&](float x) { return __builtin_amdgcn_ldexpf(x * inv, row_ref - 127); };
     const size_t out_rows = (size_t)p.batch.total * p.q_heads;
     auto out_row = [&](int r) { return (size_t)(t0 + r / p.group) * p.q_heads + head * p.group + r % p.group; };
     const int r_lane = row0 + wave * 32 + l32;
@@ -482,7 +546,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         for (int a = a0; a < a0 + 2; ++a)
 #pragma unroll
             for (int v = 0; v < 16; v += 4)
-                *reinterpret_cast<float4 *>(my_rows + l32 * kOutRow + (32 * (a - a0) + 2 * v + 4 * h32) * 4) = make_float4(o[a][v] * inv * f, o[a][v + 1] * inv * f, o[a][v + 2] * inv * f, o[a][v + 3] * inv * f);
+                *reinterpret_cast<float4 *>(my_rows + l32 * kOutRow + (32 * (a - a0) + 2 * v + 4 * h32) * 4) = make_float4(mean(o[a][v]), mean(o[a][v + 1]), mean(o[a][v + 2]), mean(o[a][v + 3]));
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {      // eight channels a lane, eight rows a time

@@ -144,3 +144,92 @@ def test_sums_of_values_keep_the_values_range(torch, KV, dim, size, new, copies,
     got, q = w.attend(normal(torch, 11, new, 4, dim), copies)
     for i in {0, 1, new - 1} & set(range(new)):
         close(w, got, q, i, i % 4)
+
+
+def close_by_block(w, got, q, i, h, **kw):
+    """As close(), where scales are so far apart that every block of 32 keys counts by itself: what may be left out is below 2^-33 of the largest weight in its block."""
+    torch = w.torch
+    keys, kh = w.seen(i, q.shape[0], kw.get("causal", True), kw.get("window", 0)), h // (q.shape[1] // w.heads)
+    scale = w.D ** -0.5 if kw.get("scale") is None else abs(kw["scale"])
+    k, v = w.k[keys, kh], w.v[keys, kh]
+    p = torch.softmax(k @ q[i, h] * scale, 0)
+    d = 2.0 ** -16 * scale * float((k.abs() @ q[i, h].abs()).max())
+    # of a weight: twice the error of its exponent, rounding to 11 bits, fp32 sums and factors; of the sum of weights the same, on what the row is
+    want = p @ v
+    tol = 2.0 ** -8 * want.abs() + (np.expm1(2 * d) + 2.0 ** -10 + 2.0 ** -14) * (p @ v.abs())
+    block = torch.arange(keys.start, keys.stop) // 32
+    for b in block.unique():
+        at = block == b
+        tol = tol + 32 * 2.0 ** -33 * p[at].max() * v[at].abs().max()
+    off = (got[i, h] - want).abs() - tol
+    assert bool((off <= 0).all()), (i, h, float(off.max()), got[i, h, :4], want[:4])
+
+
+LENGTHS = [(*FEW, 700), (*FEW, 9000), (8, 1, 2500), (3, 40, 300), (*MANY, 300), (*MANY, 6000), (300, 1, 9000)]
+
+
+@pytest.mark.parametrize("new,copies,L", LENGTHS)
+@pytest.mark.parametrize("dim,e", [(64, 18), (128, 30), (128, 40), (128, 100), (256, 60)])
+def test_loud_values_that_a_row_does_not_see_do_not_matter_to_it(torch, KV, dim, e, new, copies, L):
+    """The last 32 tokens' values are 2^e louder; tokens before them do not see them.  The last tokens do."""
+    v = normal(torch, 12, L, 1, dim)
+    v[L - 32:] *= 2.0 ** e
+    w = Sequence(torch, KV, normal(torch, 13, L, 1, dim), v * 2.0 ** -20)
+    got, q = w.attend(normal(torch, 14, new, 4, dim), copies)
+    for i in {0, 1, new // 2, new - 34, new - 33, new - 32, new - 31, new - 1} & set(range(new)):
+        close_by_block(w, got, q, i, i % 4)
+
+
+@pytest.mark.parametrize("new,copies,L", LENGTHS)
+@pytest.mark.parametrize("dim,e,window", [(64, 30, 40), (128, 40, 70), (128, 90, 120), (256, 40, 64)])
+def test_loud_values_outside_a_row_s_window_do_not_matter_to_it(torch, KV, dim, e, window, new, copies, L):
+    """Every third run of 50 tokens is louder, so that windows begin and end in them."""
+    v = normal(torch, 15, L, 1, dim)
+    v[torch.arange(L) // 50 % 3 == 1] *= 2.0 ** e
+    w = Sequence(torch, KV, normal(torch, 16, L, 1, dim), v * 2.0 ** -20)
+    got, q = w.attend(normal(torch, 17, new, 4, dim), copies, window=window)
+    for i in set(list(range(0, new, 13)) + [1, new - 2, new - 1]) & set(range(new)):
+        close_by_block(w, got, q, i, i % 4, window=window)
+
+
+@pytest.mark.parametrize("new,copies,L", LENGTHS)
+@pytest.mark.parametrize("dim,e,below", [(64, 40, 300.0), (128, 40, 27.7), (128, 24, 16.6), (128, 100, 69.3), (256, 60, 41.6)])
+@pytest.mark.parametrize("first", [True, False])
+def test_loud_values_count_by_their_weight(torch, KV, first, dim, e, below, new, copies, L):
+    """Values 2^e louder with scores `below` under the others: of no weight, or of so little that both sides count, before the others or behind them."""
+    k, v, q = normal(torch, 18, L, 1, dim) * 0.25, normal(torch, 19, L, 1, dim), normal(torch, 20, new, 2, dim) * 0.25
+    k[:, 0, 0] = 0.0
+    q[..., 0] = 8.0
+    at = slice(0, 40) if first else slice(L - new - 60, L - new - 20)
+    k[at, 0, 0] = -below * dim ** 0.5 / 8.0
+    v[at] *= 2.0 ** e
+    w = Sequence(torch, KV, k, v * 2.0 ** -20)
+    got, q = w.attend(q, copies)
+    for i in {0, new // 2, new - 1}:
+        close_by_block(w, got, q, i, i % 2)
+
+
+@pytest.mark.parametrize("new,copies,L", LENGTHS)
+@pytest.mark.parametrize("up", [True, False])
+def test_values_that_grow_or_fade_over_the_whole_range(torch, KV, up, new, copies, L):
+    run = 2.0 ** torch.linspace(-118, 118, L)[:, None, None]
+    w = Sequence(torch, KV, normal(torch, 21, L, 1, 128), normal(torch, 22, L, 1, 128) * (run if up else run.flip(0)))
+    got, q = w.attend(normal(torch, 23, new, 2, 128), copies)
+    for i in set(range(0, new, 17)) | {new - 1}:
+        close_by_block(w, got, q, i, i % 2)
+
+
+@pytest.mark.parametrize("new,copies,L", [(*FEW, 700), (*FEW, 9000), (*MANY, 300), (*MANY, 6000), (300, 1, 9000)])
+def test_far_scales_with_vectors_that_are_not_finite_and_blocks_of_zeros(torch, KV, new, copies, L):
+    """NaN for the rows that see the token, no others; zeros beside loud values stay zeros."""
+    k, v = normal(torch, 24, L, 1, 64), normal(torch, 25, L, 1, 64)
+    v[torch.arange(L) // 32 % 2 == 0] *= 2.0 ** 50
+    v[32 * 3:32 * 5] = 0.0
+    at = L - new // 2 - 1
+    v[at, 0, 7] = float("nan")
+    w = Sequence(torch, KV, k, v)
+    got, q = w.attend(normal(torch, 26, new, 2, 64), copies)
+    seeing = torch.arange(new) + L - new >= at
+    assert torch.equal(torch.isnan(got).all(-1).all(-1), seeing) and not bool(torch.isnan(got[~seeing]).any())
+    for i in {0, new // 4} & set(torch.nonzero(~seeing).flatten().tolist()):
+        close_by_block(w, got, q, i, 0)
