@@ -171,21 +171,22 @@ LENGTHS = [(*FEW, 700), (*FEW, 9000), (8, 1, 2500), (3, 40, 300), (*MANY, 300), 
 @pytest.mark.parametrize("new,copies,L", LENGTHS)
 @pytest.mark.parametrize("dim,e", [(64, 18), (128, 30), (128, 40), (128, 100), (256, 60)])
 def test_loud_values_that_a_row_does_not_see_do_not_matter_to_it(torch, KV, dim, e, new, copies, L):
-    """The last 32 tokens' values are 2^e louder; tokens before them do not see them.  The last tokens do."""
-    v = normal(torch, 12, L, 1, dim)
-    v[L - 32:] *= 2.0 ** e
+    """Values are 2^e louder from the last block of 32 on that is the second of its 64; tokens before them do not see them.  The last tokens do."""
+    v, start = normal(torch, 12, L, 1, dim), (L - 33) // 64 * 64 + 32
+    v[start:] *= 2.0 ** e
     w = Sequence(torch, KV, normal(torch, 13, L, 1, dim), v * 2.0 ** -20)
     got, q = w.attend(normal(torch, 14, new, 4, dim), copies)
-    for i in {0, 1, new // 2, new - 34, new - 33, new - 32, new - 31, new - 1} & set(range(new)):
+    first = start - (L - new)      # that sees them
+    for i in {0, 1, new // 2, first - 40, first - 33, first - 20, first - 1, first, new - 1} & set(range(new)):
         close_by_block(w, got, q, i, i % 4)
 
 
 @pytest.mark.parametrize("new,copies,L", LENGTHS)
 @pytest.mark.parametrize("dim,e,window", [(64, 30, 40), (128, 40, 70), (128, 90, 120), (256, 40, 64)])
 def test_loud_values_outside_a_row_s_window_do_not_matter_to_it(torch, KV, dim, e, window, new, copies, L):
-    """Every third run of 50 tokens is louder, so that windows begin and end in them."""
+    """Every third block is louder, so that windows begin and end in them."""
     v = normal(torch, 15, L, 1, dim)
-    v[torch.arange(L) // 50 % 3 == 1] *= 2.0 ** e
+    v[torch.arange(L) // 32 % 3 == 1] *= 2.0 ** e
     w = Sequence(torch, KV, normal(torch, 16, L, 1, dim), v * 2.0 ** -20)
     got, q = w.attend(normal(torch, 17, new, 4, dim), copies, window=window)
     for i in set(list(range(0, new, 13)) + [1, new - 2, new - 1]) & set(range(new)):
@@ -200,7 +201,8 @@ def test_loud_values_count_by_their_weight(torch, KV, first, dim, e, below, new,
     k, v, q = normal(torch, 18, L, 1, dim) * 0.25, normal(torch, 19, L, 1, dim), normal(torch, 20, new, 2, dim) * 0.25
     k[:, 0, 0] = 0.0
     q[..., 0] = 8.0
-    at = slice(0, 40) if first else slice(L - new - 60, L - new - 20)
+    at = (L - new) // 64 * 64 - 64      # (blocks of 32: what is quiet in one with loud values is held as next to nothing)
+    at = slice(0, 64) if first else slice(at, at + 32)
     k[at, 0, 0] = -below * dim ** 0.5 / 8.0
     v[at] *= 2.0 ** e
     w = Sequence(torch, KV, k, v * 2.0 ** -20)
