@@ -62,12 +62,13 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     // the lane's row and the keys [seen_lo, seen_hi) that it sees
     const int r = tile * 16 + l16 < rows ? tile * 16 + l16 : rows - 1;
     const int tok = r / p.group, qh = head * p.group + r % p.group, pos = len - n + tok;
-    const int seen_hi = p.causal ? (pos + 1 < 0 ? 0 : pos + 1) : len;
+    const auto hi_of = [&](int at) { return at < 0 ? 0 : p.causal ? at + 1 : len; };      // (a token without a position sees nothing)
+    const int seen_hi = hi_of(pos);
     const int seen_lo = p.causal && p.window > 0 && pos + 1 > p.window ? pos + 1 - p.window : 0;
     // of the tile: its first row sees the fewest and the earliest keys
     const int tok_a = tile * 16 / p.group, last = tile * 16 + 15 < rows ? tile * 16 + 15 : rows - 1, tok_z = last / p.group;
     const int pos_a = len - n + tok_a, pos_z = len - n + tok_z;
-    const int any_hi = p.causal ? (pos_z + 1 < 0 ? 0 : pos_z + 1) : len, all_hi = p.causal ? (pos_a + 1 < 0 ? 0 : pos_a + 1) : len;
+    const int any_hi = hi_of(pos_z), all_hi = hi_of(pos_a);
     const int any_lo = p.causal && p.window > 0 && pos_a + 1 > p.window ? pos_a + 1 - p.window : 0, all_lo = p.causal && p.window > 0 && pos_z + 1 > p.window ? pos_z + 1 - p.window : 0;
     const int blk0 = any_lo >> 5, blk1 = (any_hi + 31) >> 5;
     // this workgroup's blocks

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     const int len = kv_length(p.cache, p.batch, item.value), rows = n * p.group, tiles = (rows + kRows - 1) / kRows;
     if (local < 0 || local >= tiles) return;
     const int row0 = (p.causal ? tiles - 1 - local : local) * kRows;      // (causal: the rows with the most keys first)
-    auto hi_of = [&](int at) { return p.causal ? (at + 1 < 0 ? 0 : at + 1) : len; };
+    auto hi_of = [&](int at) { return at < 0 ? 0 : p.causal ? at + 1 : len; };      // (a token without a position sees nothing)
     auto lo_of = [&](int at) { return p.causal && p.window > 0 && at + 1 > p.window ? at + 1 - p.window : 0; };
     auto pos_of = [&](int row) { return len - n + (row < rows ? row : rows - 1) / p.group; };
     // keys that some row of the workgroup sees, and those that all rows of the wavefront see
