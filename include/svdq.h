@@ -418,7 +418,7 @@ typedef struct {
     const int32_t *cu_new, *kv_len, *block_table; /* device: [sequences + 1], [sequences], [sequences][table_width] */
     int sequences, table_width;
     int new_tokens; /* of all sequences */
-    int max_new;    /* no sequence has more new tokens (attention: chooses the kernels; tokens past it may be refused a row) */
+    int max_new;    /* no sequence has more new tokens (attention: chooses the kernels; of a sequence with more, the first max_new are right, and later ones right or not written) */
     int max_len;    /* no kv_len is larger (attention: how the keys are cut; larger ones are right, but slower) */
 } svdq_kv_batch;
 typedef struct {

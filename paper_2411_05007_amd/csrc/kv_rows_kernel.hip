@@ -325,7 +325,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     __syncthreads();
     // pieces of four channels of a row
     const long long part = ((long long)blockIdx.z * p.cache.heads + head) * p.chunks;      // of this row tile's parts
-    const int live_rows = rows - tile * 16 < 16 ? rows - tile * 16 : 16, pieces = live_rows * (D / 4);
+    const int live_rows = rows - tile * 16 < cap ? rows - tile * 16 : cap, pieces = live_rows * (D / 4);      // (tokens past max_new have no room, and no row)
     const size_t part_floats = (size_t)cap * (D + 2);      // [cap][D] weighted means, [cap][2] maximum and sum of weights
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.partial + part * part_floats, (size_t)nchunks * part_floats * 4);
     auto store = [&](int row, int d, kv_floatx4 x) {

@@ -55,3 +55,25 @@ def test_tokens_without_a_position_see_no_key(torch, KV, dim, new, length, copie
         alone = cache.attention(q[without:].repeat(copies, 1, 1), batch(length), causal=causal).view(copies, length, group, dim)
         assert float((out[:, without:].float() - alone.float()).abs().max()) <= 2.0 ** -7 * float(alone.float().abs().max())
         assert bool((alone != 0).any(-1).all())
+
+
+@pytest.mark.parametrize("dim,group,max_new,new,length", [
+    (128, 4, 1, 2, 500), (128, 4, 1, 2, 9000), (64, 1, 1, 3, 500), (64, 1, 1, 3, 9000), (256, 3, 2, 5, 5000), (128, 5, 3, 4, 9000), (64, 5, 4, 9, 700),
+    (128, 4, 5, 300, 700),      # two tiles of rows
+])
+def test_tokens_past_the_most_leave_the_others_right(torch, KV, dim, group, max_new, new, length):
+    """A sequence has more new tokens than the batch says that any has: the first ones are as they are in a batch that says it, the others like that or not written."""
+    cache, table = filled(torch, KV, 2, dim, length, seed=3)
+    q = torch.randn(new, 2 * group, dim, device=DEV).to(torch.bfloat16)
+    batch = lambda most: KV.KVBatch(i32(torch, [0, new]), i32(torch, [length]), table, new, most, length)
+    want = cache.attention(q, batch(new)).float()
+    workspace = torch.full((cache.attention_workspace(batch(max_new), 2 * group).numel() + 4096,), 0x5A, dtype=torch.uint8, device=DEV)
+    for _ in range(3):
+        guard = torch.full((new + 2, 2 * group, dim), 77.0, dtype=torch.bfloat16, device=DEV)
+        cache.attention(q, batch(max_new), out=guard[1:-1], workspace=workspace[:-4096])
+        torch.cuda.synchronize()
+        assert bool((guard[[0, -1]] == 77).all()) and bool((workspace[-4096:] == 0x5A).all())
+        got = guard[1:-1].float()
+        right = (got - want).abs() <= 2.0 ** -7 * want.abs().max()      # (another cut: two roundings of an output at most)
+        assert bool(right[:max_new].all())
+        assert bool((right | (got == 77))[max_new:].all())
