@@ -232,8 +232,8 @@ __device__ __forceinline__ float kv_max_lanes(float x) {
     if (U >= 16) x = kv_max_dpp<0x140>(x);          // sixteen
     return x;
 }
-// 1 / the sum of a row's weights (no key seen: zeros; NaN stays)
-__device__ __forceinline__ float kv_inverse(float sum) { return sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum; }
+// 1 / the sum of a row's weights, within an ulp (no key seen: zeros; NaN stays).  (The division proper is a chain of ten instructions, twice or three times a launch.)
+__device__ __forceinline__ float kv_inverse(float sum) { return sum > 0.f ? __builtin_amdgcn_rcpf(sum) : sum == sum ? 0.f : sum; }
 __device__ __forceinline__ float kv_sum32(float x) { float a, b; kv_swap32(x, a, b); return a + b; }
 __device__ __forceinline__ float kv_sum16(float x) { float a, b; kv_swap16(x, a, b); return a + b; }
 
