@@ -207,6 +207,17 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
         for (int j = 1; j < 8; ++j) top = fmaxf(top, t[j]);
         return kv_max32(kv_max16(top));
     };
+    auto weights = [&](const float (&t)[8], float from, float &sum) {      // and the sum of what is multiplied
+        kv_f16x8 pf;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const kv_f16x2 e = {(_Float16)__builtin_amdgcn_exp2f(t[j] - from + kShift), (_Float16)__builtin_amdgcn_exp2f(t[j + 1] - from + kShift)};
+            sum = __builtin_amdgcn_fdot2(e, kv_f16x2{(_Float16)1.f, (_Float16)1.f}, sum, false);
+            pf[j] = e[0];
+            pf[j + 1] = e[1];
+        }
+        return pf;
+    };
     auto step = [&](Block<D> &cur, int i) {
         const int vb = __builtin_amdgcn_readlane(vb_l, i);
         float t[8];
@@ -222,13 +233,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
             m = m_new;
             ref = ref_new;
         }
-        kv_f16x8 pf;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float e = __builtin_amdgcn_exp2f(t[j] - m + kShift);
-            l += e;
-            pf[j] = (_Float16)e;
-        }
+        const kv_f16x8 pf = weights(t, m, l);
         const float vf = kv_pow2(vb - ref);
 #pragma unroll
         for (int a = 0; a < D / 32; ++a) {
@@ -273,15 +278,9 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
                 load(even, i);
                 float t[8];
                 scores(even, i, t);
-                const float top = largest_of(t), from = top > -__builtin_inff() ? top : 0.f;
-                kv_f16x8 pf;
+                const float top = largest_of(t);
                 float sum = 0.f, largest = 0.f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float e = __builtin_amdgcn_exp2f(t[j] - from + kShift);
-                    sum += e;
-                    pf[j] = (_Float16)e;
-                }
+                const kv_f16x8 pf = weights(t, top > -__builtin_inff() ? top : 0.f, sum);
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d)
 #pragma unroll

@@ -235,3 +235,17 @@ def test_far_scales_with_vectors_that_are_not_finite_and_blocks_of_zeros(torch, 
     assert torch.equal(torch.isnan(got).all(-1).all(-1), seeing) and not bool(torch.isnan(got[~seeing]).any())
     for i in {0, new // 4} & set(torch.nonzero(~seeing).flatten().tolist()):
         close_by_block(w, got, q, i, 0)
+
+
+@pytest.mark.parametrize("dim,group", [(64, 4), (128, 2)])
+def test_the_weights_that_are_summed_are_those_that_are_multiplied(torch, KV, dim, group):
+    """Values of one have a mean of one, however the weights are rounded: of every chunk of the keys to what fp32 sums are off by.  (What the rounding of weights alone
+    leaves is 2^-12 where one key outweighs the others, too little to be seen in 16 bits.)"""
+    L = 9000
+    w = Sequence(torch, KV, normal(torch, 27, L, 1, dim) * 3, torch.ones(L, 1, dim))
+    batch = KV.KVBatch(w.i32([0, 1]), w.i32([L]), w.table, 1, 1, L)
+    workspace = w.cache.attention_workspace(batch, group).zero_()
+    w.attend(normal(torch, 28, 1, group, dim), workspace=workspace)
+    part = group * (dim + 2)      # floats of a chunk: means of the rows, then their maxima and sums
+    parts = workspace.view(torch.float32)[:20 * part].view(20, part)[:, :group * dim].double()
+    assert float((parts - 1).abs().max()) <= 2.0 ** -18
