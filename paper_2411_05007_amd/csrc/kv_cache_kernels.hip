@@ -8,7 +8,8 @@
 // other does, though the values of masked tokens are multiplied by zero.
 // Work split: a workgroup of four wavefronts has one block of a sequence and one to four heads in turn, two wavefronts the keys and two the values, 16 tokens each: a
 // maximum is a reduction within a wavefront and one exchange through LDS, which carries the mask of vectors that are not finite too.  One workgroup owns a block
-// of a head, so there is nothing to race with.  The rows of the next head are in flight while one is worked on.
+// of a head; within it a wavefront reads and writes the codes of its own tokens only, and the byte that the block has is read by one wavefront of a side, which tells both through
+// LDS and writes the new one behind the barrier of that exchange.  The rows of the next head are in flight while one is worked on.
 // Bound: memory (4 bytes read and 2 written per channel of a token) with many tokens, if the instructions stay few: conversions take the scale with them and two
 // numbers at a time, magnitudes of values are compared two at a time as integers, places and the rotation's cosines are found once for all heads.
 // 4 x 4608 tokens, 24 heads of 128: 83 us, 5.1 TB/s (one head a workgroup 103, three 83, six 83; scaled and converted apart 105).  For few tokens a chain of round
@@ -78,8 +79,8 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits, int old_by
 
 // A block of a sequence: tokens lo .. hi - 1 of it are new (rows row0 + lo .. of the input), 0 .. lo - 1 are there already.
 struct BlockWork { int lo, hi, blk; long long row0; };
-// What a workgroup's wavefronts tell each other: tokens whose vectors are not finite, largest magnitude (bits).
-struct Exchange { uint32_t bad[4], top[4]; };
+// What a workgroup's wavefronts tell each other: tokens whose vectors are not finite, largest magnitude (bits); of keys and of values the byte that the block has.
+struct Exchange { uint32_t bad[4], top[4]; int old_byte[2]; };
 __device__ __forceinline__ bool live(const BlockWork &w, int tok) { return tok >= w.lo && tok < w.hi; }
 __device__ __forceinline__ int readable(const BlockWork &w, int tok) { return tok < w.lo ? w.lo : tok < w.hi ? tok : w.hi - 1; }      // (a token that is not new: one that is, not used)
 
@@ -305,7 +306,8 @@ __device__ __forceinline__ void append_heads(const KvAppendParams &p, const Bloc
         uint32_t next[Side::kRaw];
         side.load(next, h + 1 < h1 ? h + 1 : h);
         const long long unit = unit0 + ((long long)(h - h0) << (p.cache.page_shift - 5));
-        const int old_byte = w.lo > 0 ? (int)scales[unit] : 0;
+        const bool tells = side.lane == 0 && (wave & 1) == 0;      // of the side's byte, old and new
+        const int held = tells && w.lo > 0 ? (int)scales[unit] : 0;
         side.load_old(unit);
         Exchange &ex = exchange[h & 1];      // (written again two heads on: behind a barrier that every wavefront enters when it has read it)
         const uint32_t bad = side.look(), most = side.largest(bad);
@@ -313,6 +315,7 @@ __device__ __forceinline__ void append_heads(const KvAppendParams &p, const Bloc
             ex.bad[wave] = bad;
             ex.top[wave] = most;
         }
+        if (tells) ex.old_byte[wave >> 1] = held;
         kv_lds_barrier();
         const uint32_t all = ex.bad[0] | ex.bad[1] | ex.bad[2] | ex.bad[3];
         if (all != 0u) {           // (what the other side found is left out of this side's maximum too)
@@ -321,9 +324,9 @@ __device__ __forceinline__ void append_heads(const KvAppendParams &p, const Bloc
             if (side.lane == 0) ex.top[wave] = again;
             kv_lds_barrier();
         }
-        const BlockScale sc = block_scale(umax(ex.top[wave & 2], ex.top[(wave & 2) + 1]), old_byte);
+        const BlockScale sc = block_scale(umax(ex.top[wave & 2], ex.top[(wave & 2) + 1]), __builtin_amdgcn_readfirstlane(ex.old_byte[wave >> 1]));
         side.write(unit, sc, all);
-        if (side.lane == 0 && (wave & 1) == 0) scales[unit] = (uint8_t)sc.byte;
+        if (tells) scales[unit] = (uint8_t)sc.byte;
 #pragma unroll
         for (int i = 0; i < Side::kRaw; ++i) side.raw[i] = next[i];
     }

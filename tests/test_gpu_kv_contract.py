@@ -77,3 +77,24 @@ def test_tokens_past_the_most_leave_the_others_right(torch, KV, dim, group, max_
         right = (got - want).abs() <= 2.0 ** -7 * want.abs().max()      # (another cut: two roundings of an output at most)
         assert bool(right[:max_new].all())
         assert bool((right | (got == 77))[max_new:].all())
+
+
+@pytest.mark.parametrize("dim,heads,sequences", [(64, 3, 5), (128, 2, 300), (256, 16, 40), (128, 8, 256)])
+def test_both_halves_of_a_block_grow_with_its_scale(torch, KV, dim, heads, sequences):
+    """17 to 31 tokens are in a block when a much louder one comes: the codes of all of them are rounded again to the new scale, whichever wavefront has them.  (One byte
+    a block, read before it is written; checked through what gather reads, against the codes' own values.)"""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(dim + heads)
+    cache, table = KV.KVCache(sequences, heads, dim, 32), torch.randperm(sequences, generator=gen, device=DEV).int()[:, None].contiguous()
+    for held in (17, 24, 31):
+        n = sequences * held
+        x = torch.randn(n, 2 * heads, dim, generator=gen, device=DEV).to(torch.bfloat16)
+        cu = np.arange(sequences + 1)
+        cache.append(x[:, :heads], x[:, heads:], KV.KVBatch(i32(torch, cu * held), i32(torch, [held] * sequences), table, n, held, held))
+        rows = KV.KVRows(i32(torch, [0] * sequences), i32(torch, cu * held), table, n)
+        before = cache.gather(rows)
+        loud = torch.full((sequences, 2 * heads, dim), 448.0 * 32, dtype=torch.bfloat16, device=DEV)      # (every block's byte becomes that of 2^5)
+        cache.append(loud[:, :heads], loud[:, heads:], KV.KVBatch(i32(torch, cu), i32(torch, [held + 1] * sequences), table, sequences, 1, held + 1))
+        for a, b, scales in zip(before, cache.gather(rows), (cache.k_scales, cache.v_scales)):
+            assert bool((scales == 127 + 5).all())
+            assert torch.equal(b.float(), (a.float() / 32).to(torch.float8_e4m3fn).float() * 32)
