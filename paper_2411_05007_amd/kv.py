@@ -6,7 +6,8 @@
     cache.append(k, v, batch, rope)                                   # keys rotated, both quantized
     out = cache.attention(q, batch, rope)                             # bf16 [tokens, q_heads, head_dim]
 
-Argument marshalling only; every call enqueues on the current stream (or the one that is given) and does not synchronise.
+Argument marshalling only; every call enqueues on the current stream (or the one that is given) and does not synchronise.  A stream that is given is the caller's to order
+behind what makes the inputs, and before what reads the results.
 """
 from __future__ import annotations
 
@@ -116,10 +117,15 @@ class KVCache:
         return _current_stream(self.device.index) if stream is None else stream.cuda_stream
 
     def _new(self, shape, dtype, stream):
-        """Memory of the current stream that a call on `stream` writes: not given out again before that stream is done with it."""
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if stream is not None:
-            t.record_stream(stream)
+        """Memory for a call on `stream`.  It is that stream's (what the current one still does with memory that it gave back does not reach it), and the caller's on the
+        current one: not given out again before both are done with it."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        current = torch.cuda.current_stream(self.device)
+        with torch.cuda.stream(stream):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        if current != stream:
+            t.record_stream(current)
         return t
 
     def append(self, k, v, batch: KVBatch, rope: Optional[Rope] = None, stream=None) -> None:

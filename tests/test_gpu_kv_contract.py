@@ -98,3 +98,46 @@ def test_both_halves_of_a_block_grow_with_its_scale(torch, KV, dim, heads, seque
         for a, b, scales in zip(before, cache.gather(rows), (cache.k_scales, cache.v_scales)):
             assert bool((scales == 127 + 5).all())
             assert torch.equal(b.float(), (a.float() / 32).to(torch.float8_e4m3fn).float() * 32)
+
+
+def test_memory_of_a_call_on_another_stream_is_not_what_this_one_still_writes(torch, KV):
+    """The current stream has a temporary to write and has given it back; a call on an idle stream must not be handed that memory."""
+    cache, table = filled(torch, KV, 2, 128, 9000, seed=5)
+    q = torch.randn(1, 8, 128, device=DEV).to(torch.bfloat16)
+    batch = KV.KVBatch(i32(torch, [0, 1]), i32(torch, [9000]), table, 1, 1, 9000)
+    rows = KV.KVRows(i32(torch, [0]), i32(torch, [0, 9000]), table, 9000)
+    want, held = cache.attention(q, batch), cache.gather(rows)
+    n = cache.attention_workspace(batch, 8).numel()
+    assert n > 4096      # (parts that meet)
+    torch.cuda.synchronize()
+    side, big = torch.cuda.Stream(), torch.randn(4096, 4096, device=DEV)
+    for _ in range(3):
+        for _ in range(8):
+            big @ big      # (the current stream is busy for a while)
+        for _ in range(2):
+            for size in (n, want.numel() * 2, held[0].numel() * 2, held[0].numel() * 2):
+                torch.full((size,), 0x41, dtype=torch.uint8, device=DEV)      # written behind that, and given back at once
+        got, (k, v) = cache.attention(q, batch, stream=side), cache.gather(rows, stream=side)
+        mine = cache.attention(q, batch, workspace=cache.attention_workspace(batch, 8, stream=side), stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(mine, want) and torch.equal(k, held[0]) and torch.equal(v, held[1])
+
+
+def test_a_call_on_a_captured_stream_is_replayed(torch, KV):
+    """Memory of a call inside a capture is the graph's, whether the stream is named or not."""
+    cache, table = filled(torch, KV, 2, 64, 3000, seed=6)
+    q = torch.randn(1, 4, 64, device=DEV).to(torch.bfloat16)
+    batch = KV.KVBatch(i32(torch, [0, 1]), i32(torch, [3000]), table, 1, 1, 3000)
+    cache.attention(q, batch)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        here = cache.attention(q, batch)
+        named = cache.attention(q, batch, stream=torch.cuda.current_stream())
+    for i in range(4):
+        q.copy_(torch.randn(1, 4, 64, device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = cache.attention(q, batch)
+        torch.cuda.synchronize()
+        assert torch.equal(here, want) and torch.equal(named, want)
