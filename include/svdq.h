@@ -446,7 +446,8 @@ int svdq_kv_append(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, c
  * is the largest among them.  A row that sees no key is zero.
  *   out: device bf16 [new_tokens][q_heads][head_dim], 16-byte aligned
  *   workspace: device, 256-byte aligned, >= svdq_kv_attention_workspace_bytes(); needs no initial contents.  Two calls that share one must be ordered on one stream.
- *   Its size: up to 34 MB for the parts of chunks, and for single tokens the fp32 sums of up to 16 rows for each sequence, key head and 4096 to 8192 keys.
+ *   Its size: up to 34 MB for the parts of chunks, and for single tokens the fp32 sums of up to 16 rows for each sequence, key head and 4096 to 8192 keys.  It grows with
+ *   sequences, max_new and max_len (or stays): what serves the largest of each serves every batch within them.
  * One kernel, or one for the sequences with chunks and one for those of single tokens; a further one adds the parts where the keys of many rows are cut.  What is
  * launched, and the cut, follow from the sizes in batch and shape and from window, so the same call gives the same bits.
  */

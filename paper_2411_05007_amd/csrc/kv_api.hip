@@ -91,7 +91,7 @@ int svdq_kv_append(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, c
 size_t svdq_kv_attention_workspace_bytes(const svdq_kv_shape *shape, int q_heads, int sequences, int max_new, int max_len) {
     if (!shape || check_shape(*shape) != SVDQ_OK || q_heads <= 0 || q_heads % shape->kv_heads != 0 || sequences < 0 || max_new < 0 || max_len < 0 || max_len > kMaxTokens)
         return 0;
-    return svdq::plan_kv_attention(sequences, shape->kv_heads, q_heads / shape->kv_heads, shape->head_dim, max_new, max_len, 0, -1).total;
+    return svdq::kv_workspace_bytes(sequences, shape->kv_heads, q_heads / shape->kv_heads, shape->head_dim, max_new, max_len);
 }
 
 int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope, const svdq_kv_rows *q, int q_heads,

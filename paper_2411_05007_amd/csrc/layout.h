@@ -816,6 +816,19 @@ inline bool kv_few_rows(int sequences, int heads, int dim, long long rows, int m
     const double many = 15000.0 + (parts > 1 ? 12000.0 : 0.0) + (rounds > 1.0 ? rounds : 1.0) * 2200.0 * (double)max_len / 64.0 / parts * dim / 128.0;
     return few <= many;
 }
+// Parts (chunks of all row tiles) that the kernel of few rows has at most: kv_chunk_blocks() cuts either into 256 of all row tiles together or into chunks of 128 blocks
+// at least.  Tiles of more than sixteen rows are held to as many as a tile of sixteen would have, or 1024.  All of it grows with each argument, so that a workspace for the
+// largest sequences, max_new and max_len is one for every smaller batch.
+inline long long kv_most_row_parts(long long wgs, int blocks) {
+    const long long pieces = (blocks + 127) / 128, parts = wgs * (pieces < kKvMostChunks ? pieces : kKvMostChunks);
+    return blocks <= 32 ? 0 : parts > 256 ? parts : 256;
+}
+inline long long kv_row_parts_limit(int sequences, int heads, long long row_tiles, int blocks) {
+    const long long all = kv_most_row_parts((long long)sequences * heads * row_tiles, blocks), one = kv_most_row_parts((long long)sequences * heads, blocks);
+    const long long held = blocks <= 32 || one > 1024 ? one : 1024;
+    return row_tiles <= 1 || all < held ? all : held;
+}
+inline size_t kv_row_part_bytes(long long parts, int cap, int dim) { return align256((size_t)parts * cap * (dim + 2) * 4) + align256((size_t)parts * 8); }
 inline void plan_kv_rows(KvPlan &p, int sequences, int heads, int dim, long long rows, int max_new, int max_len, int window) {
     p.row_tiles = (int)((rows + 15) / 16);
     p.row_cap = rows < 16 ? (int)rows : 16;
@@ -823,6 +836,11 @@ inline void plan_kv_rows(KvPlan &p, int sequences, int heads, int dim, long long
     int blocks = max_len > 0 ? (max_len + 31) / 32 : 1;
     p.chunk_blocks = kv_chunk_blocks(wgs, blocks);
     p.chunks = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
+    if (p.chunks > 1 && p.chunks * wgs > kv_row_parts_limit(sequences, heads, p.row_tiles, blocks)) {
+        const long long room = kv_row_parts_limit(sequences, heads, p.row_tiles, blocks) / wgs;
+        p.chunk_blocks = room > 1 ? (int)((blocks + room - 1) / room) : blocks;
+        p.chunks = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
+    }
     if (p.chunks > 1) {
         const size_t parts = (size_t)sequences * p.row_tiles * heads * p.chunks;
         p.few_off = p.total;
@@ -836,6 +854,21 @@ inline void plan_kv_rows(KvPlan &p, int sequences, int heads, int dim, long long
         p.chunks = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
     }
 }
+// Parts of many rows: no more than their row tiles leave room for among the slots, and no more than kKvMostParts of every row.
+inline size_t kv_tile_part_bytes(long long rows, int dim) { return align256((size_t)rows * dim * 4) + align256((size_t)rows * 8); }
+// The workspace for batches of so many sequences, new tokens and keys, and for all that have less of each: either kernel, or both.
+inline size_t kv_workspace_bytes(int sequences, int heads, int group, int dim, int max_new, int max_len) {
+    const long long rows = (long long)max_new * group, slots = dim == 256 ? 256 : 512;
+    const int blocks = max_len > 0 ? (max_len + 31) / 32 : 1, cap = rows < 16 ? (int)rows : 16;
+    size_t few = kv_row_part_bytes(kv_row_parts_limit(sequences, heads, (rows + 15) / 16, blocks), cap, dim), many = 0;
+    if (rows > 16) {
+        const double most = (double)kKvMostParts * sequences * (double)rows * heads;
+        if (kv_parts(1, slots, max_len) > 1) many = kv_tile_part_bytes(most < (double)(slots * 128) ? (long long)most : slots * 128, dim);
+        if (sequences > 1 && group <= kKvFewRows) many += kv_row_part_bytes(kv_row_parts_limit(sequences, heads, 1, blocks), kKvFewRows, dim);
+    }
+    few = few > many ? few : many;
+    return few < 256 ? 256 : few;
+}
 // tokens: new ones of all sequences, -1 if they are not known yet (the workspace for any number of them).  window: 0 or the keys that a row sees.  Neither changes
 // the kernel of the longest sequence, and a call needs no more workspace than without them.
 inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len, int window, long long tokens) {
@@ -846,7 +879,7 @@ inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, in
     p.chunks = p.parts = 1;
     if (p.few) {
         plan_kv_rows(p, sequences, heads, dim, rows, max_new, max_len, window);
-        p.total = p.total < 256 ? 256 : p.total;
+        p.total = tokens < 0 ? kv_workspace_bytes(sequences, heads, group, dim, max_new, max_len) : p.total < 256 ? 256 : p.total;
         return p;
     }
     // 256 rows, one workgroup on a CU, stage a tile of keys for twice the rows: 8192 tokens x 4 heads on 16384 keys 1530 us (128 rows: 1618), joint attention of 4608
@@ -862,9 +895,8 @@ inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, in
         const long long tiles = tokens * group / 128 + large_ones, even = sequences * ((rows + 127) / 128);      // at most so many, but for single tokens
         p.parts = kv_parts((tiles < even ? tiles : even) * heads, slots, keys);
     }
-    const double most = 16.0 * (double)most_tokens * group * heads;      // (parts x row tiles are no more than `slots`, and parts no more than 16)
-    const size_t all = tokens >= 0 ? (size_t)p.parts * tokens * heads * group : most < (double)(slots * 128) ? (size_t)most : (size_t)slots * 128;
-    if (tokens >= 0 ? p.parts > 1 : kv_parts(1, slots, keys) > 1) {
+    if (p.parts > 1) {
+        const size_t all = (size_t)p.parts * tokens * heads * group;
         p.ml_off = align256(all * dim * 4);
         p.total = p.ml_off + align256(all * 8);
     }
@@ -880,7 +912,7 @@ inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, in
         const long long few_rows = rows < kKvFewRows ? rows : kKvFewRows;
         plan_kv_rows(p, sequences, heads, dim, few_rows, (int)(few_rows / group), max_len, window);
     }
-    p.total = p.total < 256 ? 256 : p.total;
+    p.total = tokens < 0 ? kv_workspace_bytes(sequences, heads, group, dim, max_new, max_len) : p.total < 256 ? 256 : p.total;
     return p;
 }
 

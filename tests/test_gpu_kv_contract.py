@@ -141,3 +141,16 @@ def test_a_call_on_a_captured_stream_is_replayed(torch, KV):
         want = cache.attention(q, batch)
         torch.cuda.synchronize()
         assert torch.equal(here, want) and torch.equal(named, want)
+
+
+@pytest.mark.parametrize("dim,heads,group", [(128, 8, 4), (64, 2, 8), (256, 1, 3)])
+def test_one_workspace_serves_every_batch_within_its_own(torch, KV, dim, heads, group):
+    cache, table = filled(torch, KV, heads, dim, 8300, seed=7)
+
+    def batch(sequences, new, length):
+        return KV.KVBatch(i32(torch, np.arange(sequences + 1) * new), i32(torch, [length] * sequences), table.expand(sequences, -1).contiguous(), sequences * new, new, length)
+    workspace = cache.attention_workspace(batch(5, 120, 8277), heads * group)
+    for sequences, new, length in ((1, 1, 8180), (5, 1, 8277), (2, 1, 4000), (3, 1, 4000), (1, 120, 8277), (5, 120, 8277), (4, 30, 8000), (1, 7, 5000), (2, 60, 1030), (3, 5, 2500)):
+        q = torch.randn(sequences * new, heads * group, dim, device=DEV).to(torch.bfloat16)
+        b = batch(sequences, new, length)
+        assert torch.equal(cache.attention(q, b, workspace=workspace), cache.attention(q, b))
