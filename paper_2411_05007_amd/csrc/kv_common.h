@@ -194,12 +194,6 @@ struct KvRotating {
         }
     }
 };
-template <int N, typename Place>
-__device__ __forceinline__ void kv_rotated(const uint16_t *row, const KvRope &rope, int pos, Place place, float (&x)[N][8]) {
-    KvRotating<N> t;
-    t.request(row, rope, pos, place);
-    t.finish(rope, place, x);
-}
 // Barrier of a workgroup for what its wavefronts wrote to LDS: loads from memory stay in flight.
 __device__ __forceinline__ void kv_lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
