@@ -364,11 +364,13 @@ __device__ __forceinline__ uint32_t bf16_pair(uint32_t w, float scale, bool high
 template <int D>
 __global__ __launch_bounds__(128) void kv_gather_kernel(KvGatherParams p) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const KvItem item = kv_item(p.batch, blockIdx.x, [](int n, int value) {
-        const long long start = value < 0 ? 0 : value;
+    // (past 2^30 no table names a page: places of tokens stay within 32 bits)
+    const auto start_of = [](int value) { return kv_within(value, 0, 1 << 30); };
+    const KvItem item = kv_item(p.batch, blockIdx.x, [&](int n, int value) {
+        const long long start = start_of(value);
         return n > 0 ? (int)((start + n + 31) / 32 - start / 32) : 0;
     });
-    const int b = item.sequence, local = item.local, r0 = item.first, n = item.count, start = item.value < 0 ? 0 : item.value;
+    const int b = item.sequence, local = item.local, r0 = item.first, n = item.count, start = start_of(item.value);
     const int blk = (start >> 5) + local;
     const long long end = (long long)start + n;
     if (local < 0 || n == 0 || (long long)blk * kKvBlock >= end) return;

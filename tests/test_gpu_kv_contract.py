@@ -154,3 +154,13 @@ def test_one_workspace_serves_every_batch_within_its_own(torch, KV, dim, heads, 
         q = torch.randn(sequences * new, heads * group, dim, device=DEV).to(torch.bfloat16)
         b = batch(sequences, new, length)
         assert torch.equal(cache.attention(q, b, workspace=workspace), cache.attention(q, b))
+
+
+def test_gather_of_tokens_past_any_table_is_zeros(torch, KV):
+    cache, table = filled(torch, KV, 2, 64, 200, seed=8)
+    for first in (2 ** 31 - 1, 2 ** 31 - 40, 2 ** 30 + 5, 2 ** 30 - 7, 256):
+        guard = [torch.full((104, 2, 64), 9.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        cache.gather(KV.KVRows(i32(torch, [first, 0]), i32(torch, [0, 70, 100]), table.expand(2, -1).contiguous(), 100), out=[g[2:-2] for g in guard])
+        held = cache.gather(KV.KVRows(i32(torch, [0]), i32(torch, [0, 30]), table, 30))
+        for g, h in zip(guard, held):
+            assert bool((g[:2] == 9).all()) and bool((g[-2:] == 9).all()) and bool((g[2:72] == 0).all()) and torch.equal(g[72:102], h)
