@@ -8,14 +8,14 @@
 // two such products the operand of the next), the block's scale in one factor per row; running maximum and sum per row in fp32; P^T in f16;
 // O^T += V^T P^T with the values as code * 2^(byte - reference), the reference exponent the largest so far, which is exact while the wavefront's bytes are at most
 // 15 apart (kv_common.h has the other way).  P is scaled by 2^8 (and may reach 2^14
-// before the maximum is renewed), so that f16 keeps eleven bits of weights down to 2^-22 of the largest; f16 for Q, scaled by a power of two per
-// row, for the same eleven bits.
+// before the maximum is renewed), so that f16 keeps eleven bits of weights down to 2^-22 of the largest (those below 2^-33 are zero); f16 for Q, scaled by a power of two per
+// row, for the same eleven bits down to 2^-28 of the row's largest.
 // Loads: the pages and scale bytes of a wavefront's next 64 blocks are looked up at once, one in a lane; the codes of two blocks are in flight (16 KB a
 // wavefront, three workgroups a CU), each requested right behind the last use of its registers.
-// The wavefronts' sums meet in LDS.  With several chunks the parts lie in the workspace, past the L2s, and the workgroup that finds all of its row tile
-// arrived adds them in chunk order (the same bits whoever it is), eight requests in flight a thread; nothing waits for another workgroup.
+// The wavefronts meet in LDS, as weighted means.  With several chunks the parts lie in the workspace, past the L2s, and the workgroup that finds all of its row tile
+// arrived joins them in chunk order (the same bits whoever it is), eight requests in flight a thread; nothing waits for another workgroup.
 // Bound: memory, one byte per channel of a key and a value: one sequence of 131071 keys, 8 key heads of 128, 32 query heads 54 us (5.0 TB/s), 64 sequences
-// of 100 to 16384 keys 255 us (4.5 TB/s).  Short ones by a chain of round trips: 5.7 us for one block (lengths, table, codes, queries turned on the way), 9.5 us for 777 keys of eight
+// of 100 to 16384 keys 245 us (4.65 TB/s).  Short ones by a chain of round trips: 5.7 us for one block (lengths, table, codes, queries turned on the way), 9.3 us for 777 keys of eight
 // heads, where the eight CUs draw 52 GB/s each.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -8,12 +8,12 @@
 // reference exponent the largest so far, while the bytes are at most 15 apart: kv_common.h has the other way) and laid out as operands, so that an operand read is 64 lanes x 16 bytes in a row.  S^T = K Q^T by
 // v_mfma_f32_32x32x16_f16: a lane has one row of queries, its accumulators are the operand of O^T = V^T P^T as they stand, and maximum and sum of a row are one exchange
 // between lane halves away.  Statistics in fp32; P is exp2(t - m + 8) in f16, at most 2^14 before the maximum is renewed, so weights down to 2^-22 of the
-// largest keep eleven bits; Q in f16, scaled by a power of two per row, for the same eleven bits.
+// largest keep eleven bits and those below 2^-33 are zero; Q in f16, scaled by a power of two per row, for the same eleven bits down to 2^-28 of the row's largest.
 // The scores of a tile are made beside the weights of the one before, codes are requested two and three tiles ahead, pages and scale bytes 32 tiles ahead; one barrier a tile.
 // Few row tiles on many keys take parts of the keys, which kv_meet_kernel joins.  A wavefront whose rows are past the sequence's only carries codes.
-// Bound: matrix cores and vector ALU, which overlap little, at the chip's power limit (2.05 of 2.4 GHz).  8192 tokens, 32 query heads on 8, on 16384 keys 1530 us, 1.08 PFLOP/s
-// (a library product of 8192 cubed in f16 reaches 1.215): matrix cores busy 52 % of the time, vector ALU 55 %; 4608 tokens of 24 heads, all with all, 279 us, 49 and 54 %, and 432
-// tiles are two rounds of 256 CUs; six ragged chunks of up to 2111 tokens 355 us, 43 and 57 %.  What a workgroup of 128 rows costs beside its tiles (1.05 us each): scan over
+// Bound: matrix cores and vector ALU, which overlap little, at the chip's power limit (1.9 of 2.4 GHz under the profiler).  8192 tokens, 32 query heads on 8, on 16384 keys 1540 us, 1.07 PFLOP/s
+// (a library product of 8192 cubed in f16 reaches 1.215): matrix cores busy 51 % of the time, vector ALU 55 %; 4608 tokens of 24 heads, all with all, 280 us, 48 and 54 %, and 432
+// tiles are two rounds of 256 CUs; six ragged chunks of up to 2111 tokens 350 us, 43 and 58 %; heads of 64, 8192 tokens on 16384 keys 1036 us, 34 and 68 %.  What a workgroup of 128 rows costs beside its tiles (1.05 us each): scan over
 // the sequences 1.2 us, queries and first pages 2.2, turning 2.5, first codes 1.4, out 2, of which the other workgroup of the CU covers about two thirds.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

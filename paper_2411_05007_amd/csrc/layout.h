@@ -902,8 +902,8 @@ inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, in
     }
     // Single tokens beside chunks go to the kernel of few, in a launch of their own, where that is estimated to cost less (us; a row tile costs a CU 5 and 1.05 for 64 keys), or
     // where a lone workgroup would walk the longest sequence for 60 us.  Together | apart, us (8 key heads of 128, 32 query heads): 512 tokens on 4512 beside seven single
-    // ones on 32000 keys 623 | 137, beside three on 100000 1935 | 166, beside 31 on 16000 350 | 194, beside seven on 1500 63 | 78; 256 beside 63 on 500 32 | 26, on 4000
-    // 106 | 69; 2048 on 2048 beside 31 on 4000 131 | 83, on 500 59 | 68.  Not mixed: 64 sequences of 1 to 16 tokens on up to 4000 keys 100 | 149.
+    // ones on 32000 keys 297 | 164, beside three on 100000 694 | 202, beside 31 on 16000 312 | 257, beside seven on 1500 71 | 80; 256 beside 63 on 500 34 | 30, on 4000
+    // 150 | 117; 2048 on 2048 beside 31 on 4000 138 | 101, on 500 62 | 70 (which the estimate gets wrong).  Not mixed: 64 sequences of 1 to 16 tokens on up to 4000 keys.
     const double tile_us = 5.0 + 1.05 * (double)keys / 64.0 * dim / 128.0, rounds = (double)tokens * group / 128.0 * heads / 256.0;
     const double together = (rounds + (double)sequences * heads / 256.0) * tile_us;
     const double apart = (rounds + (double)large_ones * heads / 256.0) * tile_us + 10.0 + 0.75e-3 * sequences * heads * (double)keys / 32.0 * dim / 128.0;
