@@ -400,7 +400,7 @@ int svdq_w8a8_debug_act(const svdq_layer_dev *layer, const void *workspace, int 
  * alignment (multiples of 8 elements), such as the columns of a fused QKV output.  Everything is enqueued on hip_stream; nothing is
  * allocated or synchronised.  SVDQ_EINVAL: a null or misaligned pointer, a negative size or stride, a stride off 8, window < 0, q_heads not a multiple
  * of kv_heads.  SVDQ_EUNSUPPORTED: another head_dim or page size, more than 2^30 tokens of a sequence, 65535 heads or sequences, a token
- * stride of 2^25 elements, or 2^31 - 1 work items.  SVDQ_ENOSPACE: a workspace smaller than the size query says.
+ * stride of 2^25 elements, or 2^31 - 1 work items.  SVDQ_ENOSPACE: a workspace smaller than the size query says for the batch.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct {
     int kv_heads, head_dim, page_tokens;

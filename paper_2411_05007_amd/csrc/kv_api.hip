@@ -110,7 +110,8 @@ int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch
     const svdq::KvPlan plan = svdq::plan_kv_attention(batch->sequences, s.kv_heads, q_heads / s.kv_heads, s.head_dim, batch->max_new, batch->max_len, causal ? window : 0,
                                                           batch->new_tokens);
     if (plan.few && (long long)batch->sequences * plan.row_tiles > kMaxGridY) return SVDQ_EUNSUPPORTED;
-    if (workspace_bytes < plan.total) return SVDQ_ENOSPACE;
+    // (the size that the query gives, of which a call with fewer tokens or a window may need less: what is refused does not hang on those)
+    if (workspace_bytes < svdq::kv_workspace_bytes(batch->sequences, s.kv_heads, q_heads / s.kv_heads, s.head_dim, batch->max_new, batch->max_len)) return SVDQ_ENOSPACE;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     svdq::KvAttentionParams p{};
     p.cache = cache_of(cache);
