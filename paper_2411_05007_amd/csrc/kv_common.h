@@ -226,6 +226,7 @@ __device__ __forceinline__ float kv_max_lanes(float x) {
     if (U >= 16) x = kv_max_dpp<0x140>(x);          // sixteen
     return x;
 }
+__device__ __forceinline__ float kv_within_range(float x) { return __builtin_elementwise_maximum(__builtin_elementwise_minimum(x, 3.4028235e38f), -3.4028235e38f); }      // (NaN stays)
 // 1 / the sum of a row's weights, within an ulp (no key seen: zeros; NaN stays).  (The division proper is a chain of ten instructions, twice or three times a launch.)
 __device__ __forceinline__ float kv_inverse(float sum) { return sum > 0.f ? __builtin_amdgcn_rcpf(sum) : sum == sum ? 0.f : sum; }
 __device__ __forceinline__ float kv_sum32(float x) { float a, b; kv_swap32(x, a, b); return a + b; }

@@ -182,7 +182,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
                 s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_f16_of(cur.k[j][c].z, cur.k[j][c].w, 1.f), qf[2 * c + 1], s[j], 0, 0, 0);
             }
         // the lane's eight tokens are those of slot q4
-        const float f = to_t * kv_pow2(kb - 127);
+        const float f = kv_within_range(to_t * kv_pow2(kb - 127));      // (a sum of zero times it is zero)
 #pragma unroll
         for (int j = 0; j < 8; ++j) t[j] = s[j / 4][j % 4] * f;
         if (!named || blk * kKvBlock < all_lo || blk * kKvBlock + kKvBlock > all_hi) {

@@ -284,8 +284,8 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
             largest(s, top);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {      // (not zero, so that what is masked stays masked)
-            kf[i] = to_t * kv_pow2(f.kb[i] - 127);
+        for (int i = 0; i < 2; ++i) {      // (not zero, so that what is masked stays masked; not infinite, so that a sum of zero is a score of zero)
+            kf[i] = kv_within_range(to_t * kv_pow2(f.kb[i] - 127));
             kf[i] = kf[i] < 1.1754944e-38f ? 1.1754944e-38f : kf[i];
         }
         const float most = kv_max32(__builtin_elementwise_maximum(top[0] * kf[0], top[1] * kf[1]));
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
                 const uint2 w = *reinterpret_cast<const uint2 *>(k + 16 * c);
                 s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv_f16_of(w.x, w.y, 1.f), qf[c], s, 0, 0, 0);
             }
-            const float f = to_t * kv_pow2((int)p.cache.ks[unit] - 127);
+            const float f = kv_within_range(to_t * kv_pow2((int)p.cache.ks[unit] - 127));
             float top = -__builtin_inff();
 #pragma unroll
             for (int i = 0; i < 16; ++i) {

@@ -249,3 +249,16 @@ def test_the_weights_that_are_summed_are_those_that_are_multiplied(torch, KV, di
     part = group * (dim + 2)      # floats of a chunk: means of the rows, then their maxima and sums
     parts = workspace.view(torch.float32)[:20 * part].view(20, part)[:, :group * dim].double()
     assert float((parts - 1).abs().max()) <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("new,copies,L", [(*FEW, 300), (*FEW, 9000), (*MANY, 300), (300, 1, 9000)])
+@pytest.mark.parametrize("apart", [False, True])
+def test_large_channels_of_queries_where_keys_have_none(torch, KV, apart, new, copies, L):
+    """Queries of 1e30 and keys of 1e17 in different channels: every score is zero, though the product of their scales is past fp32.  (apart: blocks of 32 by themselves.)"""
+    k, q, v = torch.zeros(L, 1, 64), torch.zeros(new, 4, 64), normal(torch, 29, L, 1, 64)
+    k[:, :, 7], q[:, :, 9] = 1e17, 1e30
+    v[torch.arange(L) // 32 % 2 == 1] *= 2.0 ** (30 if apart else 1)
+    w = Sequence(torch, KV, k, v)
+    got, q = w.attend(q, copies)
+    for i in {0, new // 2, new - 1}:
+        (close_by_block if apart else close)(w, got, q, i, i % 4)
