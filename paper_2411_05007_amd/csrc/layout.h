@@ -805,6 +805,8 @@ inline int kv_parts(long long wgs, long long slots, long long keys) {
 // 2.2 us for each 64 keys of a round of workgroups.  Measured, us, few | many: 64 sequences of 64 rows (eight key heads) on 4000 keys 169 | 150, of 128
 // rows 298 | 155, eight sequences of 64 rows 29 | 41, of 256 rows 75 | 57, one of 256 rows on 16000 keys 58 | 74, on 500 12 | 22; four of 128 rows (24
 // heads) on 1128 keys 25 | 34; 16 of 256 rows (16 heads of 64) on 512 keys 36 | 24.
+// Heads of 64, and of 256: 64 sequences of 64 rows on 4000 keys 85 | 100, 408 | 307 (the two that the estimate gets wrong), of 128 rows 155 | 110, 847 | 388; eight of 64 rows 20 | 27,
+// 51 | 57; one of 256 rows on 16000 keys 33 | 42, 115 | 105; 200 of 32 rows on 1000 keys 47 | 87, 259 | 324.
 inline bool kv_few_rows(int sequences, int heads, int dim, long long rows, int max_len) {
     const long long tiles = (rows + 15) / 16, blocks = (max_len + 31) / 32;
     if (rows <= 16) return true;
