@@ -396,10 +396,14 @@ int svdq_w8a8_debug_act(const svdq_layer_dev *layer, const void *workspace, int 
  * of each position; dims a multiple of 16 up to head_dim.  Pairs (i, i + dims / 2), or (2 i, 2 i + 1) if interleaved:
  * (a, b) -> (a cos - b sin, b cos + a sin) in fp32; channels from dims on stay.  A position past the table takes its last row.
  *
+ * The norm (svdq_kv_norm, NULL for none), before the rotation: y = w x / sqrt(mean x^2 + eps) over a head's channels, in fp32, not rounded in between.  Weights:
+ * device fp32, 16-byte aligned, head_dim of them for all heads or, with per_head, for each one (q_heads rows for queries, kv_heads for keys); NULL: ones.  Tokens at
+ * positions below first_tokens take the weights q_first and k_first (the text tokens of a joint block).  eps is at least 1e-30.
+ *
  * head_dim is 64, 128 or 256.  All inputs are bf16 with channels next to each other and any token and head stride that keeps 16-byte
  * alignment (multiples of 8 elements), such as the columns of a fused QKV output.  Everything is enqueued on hip_stream; nothing is
- * allocated or synchronised.  SVDQ_EINVAL: a null or misaligned pointer, a negative size or stride, a stride off 8, window < 0, q_heads not a multiple
- * of kv_heads.  SVDQ_EUNSUPPORTED: another head_dim or page size, more than 2^30 tokens of a sequence, 65535 heads or sequences, a token
+ * allocated or synchronised.  SVDQ_EINVAL: a null or misaligned pointer, a negative size or stride, a stride off 8, window, sinks or first_tokens < 0, an eps that is not
+ * finite or below 1e-30, q_heads not a multiple of kv_heads.  SVDQ_EUNSUPPORTED: another head_dim or page size, more than 2^30 tokens of a sequence, 65535 heads or sequences, a token
  * stride of 2^25 elements, or 2^31 - 1 work items.  SVDQ_ENOSPACE: a workspace smaller than the size query says for the batch.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct {
@@ -429,12 +433,21 @@ typedef struct {
     const void *data; /* device bf16 [tokens][heads][head_dim] with the strides below, in elements */
     int64_t token_stride, head_stride;
 } svdq_kv_rows;
+typedef struct {
+    const float *q_weight, *k_weight; /* device */
+    const float *q_first, *k_first;   /* device: of tokens at positions below first_tokens */
+    int first_tokens, per_head;
+    float eps;
+} svdq_kv_norm;
 
 int svdq_kv_cache_sizes(const svdq_kv_shape *shape, int pages, svdq_kv_sizes *out);
 
 /* Writes the batch's new keys (rotated) and values into the cache.  One kernel; appending the same tokens again gives the same bytes. */
 int svdq_kv_append(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope,
                    const svdq_kv_rows *k, const svdq_kv_rows *v, void *hip_stream);
+/* The same with the keys normalised before they are rotated. */
+int svdq_kv_append_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_norm *norm, const svdq_kv_rope *rope,
+                          const svdq_kv_rows *k, const svdq_kv_rows *v, void *hip_stream);
 
 /*
  * Attention of the batch's new tokens over the cache, which holds them already:
@@ -455,6 +468,13 @@ size_t svdq_kv_attention_workspace_bytes(const svdq_kv_shape *shape, int q_heads
 int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope, const svdq_kv_rows *q,
                       int q_heads, float scale, int causal, int window, void *out, void *workspace, size_t workspace_bytes,
                       void *hip_stream);
+/*
+ * The same with the queries normalised before they are rotated, and with first tokens that stay visible: with causal and window > 0, position p also sees the
+ * positions below `sinks` (of 0 .. p), however far back they are; otherwise sinks changes nothing.  Blocks that no row sees are not read.
+ */
+int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_norm *norm, const svdq_kv_rope *rope,
+                             const svdq_kv_rows *q, int q_heads, float scale, int causal, int window, int sinks, void *out, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
 
 /*
  * Rows of the cache as bf16 [rows][kv_heads][head_dim] (16-byte aligned; either output may be NULL): sequence b's tokens first_token[b] ..

@@ -218,6 +218,12 @@ struct KvRope {
     const float *table;      // [positions][dims]: dims / 2 cosines, dims / 2 sines
     int positions, dims, interleaved;       // dims = 0: no rotation
 };
+struct KvNorm {              // of one side, queries or keys: x / sqrt(mean x^2 + eps) times weights, over a head's channels
+    const float *weight, *first;      // fp32 [dim] of all tokens but the first, of the first tokens of a sequence; null: ones
+    int head_stride, first_tokens;    // 0, or dim where every head has weights of its own
+    float eps;
+    int on;
+};
 struct KvRows {              // bf16 [token][head][dim], strides in elements
     const uint16_t *data;
     long long token_stride, head_stride;
@@ -227,6 +233,7 @@ struct KvAppendParams {
     KvBatch batch;
     KvRope rope;
     KvRows k, v;
+    KvNorm norm;             // of the keys
 };
 hipError_t launch_kv_append(const KvAppendParams &p, hipStream_t stream);
 struct KvGatherParams {
@@ -244,6 +251,8 @@ struct KvAttentionParams {
     int q_heads, group;      // group = q_heads / cache.heads
     float scale;             // of the scores, times log2(e)
     int causal, window;      // window = 0: none
+    KvNorm norm;             // of the queries
+    int sinks;               // with a window: first tokens of a sequence that every row at or behind them sees
     int least_rows, most_rows;     // sequences with fewer rows a head are not for the many-row kernel, those with more not for the few-row kernel
     int tile_rows, parts;    // many-row kernel: rows of a workgroup (128 or 256), parts that the keys of a row tile are cut into
     int row_tiles;           // few-row kernel: tiles of 16 rows a sequence and head may need

@@ -58,6 +58,14 @@ svdq::KvBatch batch_of(const svdq_kv_batch *b) { return svdq::KvBatch{b->cu_new,
 svdq::KvRope rope_of(const svdq_kv_rope *r) {
     return r ? svdq::KvRope{r->table, r->positions, r->dims, r->interleaved != 0} : svdq::KvRope{nullptr, 0, 0, 0};
 }
+int check_norm(const svdq_kv_norm *n) {
+    if (!n) return SVDQ_OK;
+    if (((uintptr_t)n->q_weight | (uintptr_t)n->k_weight | (uintptr_t)n->q_first | (uintptr_t)n->k_first) & 15) return SVDQ_EINVAL;
+    return n->first_tokens < 0 || !(n->eps >= 1e-30f && n->eps <= 3.4028235e38f) ? SVDQ_EINVAL : SVDQ_OK;
+}
+svdq::KvNorm norm_of(const svdq_kv_norm *n, const float *weight, const float *first, int dim) {
+    return svdq::KvNorm{weight, first, n->per_head ? dim : 0, n->first_tokens, n->eps, 1};
+}
 svdq::KvRows rows_of(const svdq_kv_rows *r) { return svdq::KvRows{static_cast<const uint16_t *>(r->data), r->token_stride, r->head_stride}; }
 int done(hipError_t e) { return e == hipSuccess ? SVDQ_OK : svdq::record_hip_error(e); }
 
@@ -76,15 +84,22 @@ int svdq_kv_cache_sizes(const svdq_kv_shape *shape, int pages, svdq_kv_sizes *ou
 
 int svdq_kv_append(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope, const svdq_kv_rows *k,
                    const svdq_kv_rows *v, void *hip_stream) {
+    return svdq_kv_append_normed(cache, batch, nullptr, rope, k, v, hip_stream);
+}
+
+int svdq_kv_append_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_norm *norm, const svdq_kv_rope *rope, const svdq_kv_rows *k,
+                          const svdq_kv_rows *v, void *hip_stream) {
     int st = check_cache(cache);
     if (st != SVDQ_OK) return st;
     if (!batch) return SVDQ_EINVAL;
     st = check_tables(batch->cu_new, batch->kv_len, batch->block_table, batch->sequences, batch->table_width, batch->new_tokens, cache->shape.page_tokens);
     if (st != SVDQ_OK) return st;
     if ((st = check_rope(rope, cache->shape.head_dim)) != SVDQ_OK) return st;
+    if ((st = check_norm(norm)) != SVDQ_OK) return st;
     if (batch->sequences == 0 || batch->new_tokens == 0) return SVDQ_OK;
     if ((st = check_rows(k)) != SVDQ_OK || (st = check_rows(v)) != SVDQ_OK) return st;
-    const svdq::KvAppendParams p{cache_of(cache), batch_of(batch), rope_of(rope), rows_of(k), rows_of(v)};
+    svdq::KvAppendParams p{cache_of(cache), batch_of(batch), rope_of(rope), rows_of(k), rows_of(v), {}};
+    if (norm) p.norm = norm_of(norm, norm->k_weight, norm->k_first, cache->shape.head_dim);
     return done(svdq::launch_kv_append(p, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -96,19 +111,28 @@ size_t svdq_kv_attention_workspace_bytes(const svdq_kv_shape *shape, int q_heads
 
 int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_rope *rope, const svdq_kv_rows *q, int q_heads,
                       float scale, int causal, int window, void *out, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    return svdq_kv_attention_normed(cache, batch, nullptr, rope, q, q_heads, scale, causal, window, 0, out, workspace, workspace_bytes, hip_stream);
+}
+
+int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, const svdq_kv_norm *norm, const svdq_kv_rope *rope, const svdq_kv_rows *q,
+                             int q_heads, float scale, int causal, int window, int sinks, void *out, void *workspace, size_t workspace_bytes, void *hip_stream) {
     int st = check_cache(cache);
     if (st != SVDQ_OK) return st;
     const svdq_kv_shape &s = cache->shape;
-    if (!batch || q_heads <= 0 || q_heads % s.kv_heads != 0 || window < 0 || batch->max_new < 0 || batch->max_len < 0) return SVDQ_EINVAL;
+    if (!batch || q_heads <= 0 || q_heads % s.kv_heads != 0 || window < 0 || sinks < 0 || batch->max_new < 0 || batch->max_len < 0) return SVDQ_EINVAL;
     st = check_tables(batch->cu_new, batch->kv_len, batch->block_table, batch->sequences, batch->table_width, batch->new_tokens, s.page_tokens);
     if (st != SVDQ_OK) return st;
-    if ((st = check_rope(rope, s.head_dim)) != SVDQ_OK) return st;
+    if ((st = check_rope(rope, s.head_dim)) != SVDQ_OK || (st = check_norm(norm)) != SVDQ_OK) return st;
     if (batch->sequences == 0 || batch->new_tokens == 0) return SVDQ_OK;
     if ((st = check_rows(q)) != SVDQ_OK) return st;
     if (!out || ((uintptr_t)out & 15) || !workspace || ((uintptr_t)workspace & 255)) return SVDQ_EINVAL;
     if (batch->max_len > kMaxTokens || (long long)batch->new_tokens * (q_heads / s.kv_heads) > 0x7fffffffll - (1 << 20)) return SVDQ_EUNSUPPORTED;
-    const svdq::KvPlan plan = svdq::plan_kv_attention(batch->sequences, s.kv_heads, q_heads / s.kv_heads, s.head_dim, batch->max_new, batch->max_len, causal ? window : 0,
-                                                          batch->new_tokens);
+    if (!causal || window == 0) sinks = 0;
+    if (sinks > kMaxTokens) sinks = kMaxTokens;
+    // (keys that a row sees: whole blocks of the first ones, where a window is)
+    const long long wide = causal ? (long long)window + ((sinks + 31) & ~31) : 0;
+    const svdq::KvPlan plan = svdq::plan_kv_attention(batch->sequences, s.kv_heads, q_heads / s.kv_heads, s.head_dim, batch->max_new, batch->max_len,
+                                                      wide > 0x7fffffffll ? 0x7fffffff : (int)wide, batch->new_tokens);
     if (plan.few && (long long)batch->sequences * plan.row_tiles > kMaxGridY) return SVDQ_EUNSUPPORTED;
     // (the size that the query gives, of which a call with fewer tokens or a window may need less: what is refused does not hang on those)
     if (workspace_bytes < svdq::kv_workspace_bytes(batch->sequences, s.kv_heads, q_heads / s.kv_heads, s.head_dim, batch->max_new, batch->max_len)) return SVDQ_ENOSPACE;
@@ -124,6 +148,8 @@ int svdq_kv_attention(const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch
     p.scale = scale * 1.4426950408889634f;      // exp(x) = exp2(x log2(e))
     p.causal = causal != 0;
     p.window = window;
+    p.sinks = sinks;
+    if (norm) p.norm = norm_of(norm, norm->q_weight, norm->q_first, s.head_dim);
     p.tile_rows = plan.tile_rows;
     p.parts = plan.parts;
     p.row_tiles = plan.row_tiles;

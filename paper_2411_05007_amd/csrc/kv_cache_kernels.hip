@@ -86,7 +86,7 @@ __device__ __forceinline__ int readable(const BlockWork &w, int tok) { return to
 
 // The keys of half a block, 16 tokens.  A unit is 16 channels of a token, the two runs of eight that the rotation pairs; a lane has N of them.
 // (Per head and wavefront the instructions are what counts: places are found once for all heads, relative to a base that is the same for all lanes.)
-template <int D>
+template <int D, bool NORM>
 struct KeySide {
     static constexpr int U = D / 16, N = U / 4, kRaw = N * 8;
     const KvAppendParams &p;
@@ -96,6 +96,7 @@ struct KeySide {
     uint32_t from[N][2], to[N][2];      // places in the rows, from there, and in the codes of a block
     uint32_t raw[kRaw];
     float c[N][8], s[N][8], x[N][2][8];
+    float weight[NORM ? N : 1][2][8];      // of the norm
     float top[N];
     __device__ __forceinline__ int token(int i) const { return 16 * half + (lane + 64 * i) / U; }
     __device__ __forceinline__ KeySide(const KvAppendParams &p_, const BlockWork &w_, int lane_, int half_) : p(p_), w(w_), lane(lane_), half(half_) {
@@ -112,7 +113,22 @@ struct KeySide {
             }
         }
     }
-    __device__ __forceinline__ void load_common() {      // the same for all heads
+    __device__ __forceinline__ void load_weights(int h) {
+#pragma unroll
+        for (int i = 0; i < (NORM ? N : 0); ++i) {
+            const int pr = (lane + 64 * i) % U, pos = w.blk * kKvBlock + readable(w, token(i));
+            const bool halves = !p.rope.interleaved && pr < p.rope.dims / 16;
+            const float *row = kv_norm_row(p.norm, pos, h);
+            kv_load_weights(row, halves ? pr * 8 : pr * 16, weight[NORM ? i : 0][0]);
+            kv_load_weights(row, halves ? pr * 8 + p.rope.dims / 2 : pr * 16 + 8, weight[NORM ? i : 0][1]);
+        }
+    }
+    // what is each head's own, once the last one's is used
+    __device__ __forceinline__ void load_next(int h) {
+        if (NORM && p.norm.head_stride != 0) load_weights(h);
+    }
+    __device__ __forceinline__ void load_common(int h0) {      // the same for all heads
+        load_weights(h0);
         if (p.rope.dims == 0) return;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -140,6 +156,7 @@ struct KeySide {
         for (int i = 0; i < N; ++i) {
             kv_floats(make_uint4(raw[i * 8], raw[i * 8 + 1], raw[i * 8 + 2], raw[i * 8 + 3]), x[i][0]);
             kv_floats(make_uint4(raw[i * 8 + 4], raw[i * 8 + 5], raw[i * 8 + 6], raw[i * 8 + 7]), x[i][1]);
+            if (NORM) kv_normalise<U>(x[i], weight[NORM ? i : 0], p.norm.eps);
             if ((lane + 64 * i) % U < p.rope.dims / 16) {
                 if (p.rope.interleaved) {
 #pragma unroll
@@ -225,7 +242,8 @@ struct ValueSide {
             if (token(j) < w.lo) keep[j >> 2] |= 0xffu << (8 * (j & 3));
         }
     }
-    __device__ __forceinline__ void load_common() {}
+    __device__ __forceinline__ void load_common(int) {}
+    __device__ __forceinline__ void load_next(int) {}
     __device__ __forceinline__ void load(uint32_t (&r)[kRaw], int h) const {
         const uint16_t *head = base + h * p.v.head_stride;
 #pragma unroll
@@ -299,7 +317,7 @@ template <typename Side>
 __device__ __forceinline__ void append_heads(const KvAppendParams &p, const BlockWork &w, int sequence, int h0, int h1, uint8_t *scales, int wave, Exchange (&exchange)[2]) {
     Side side(p, w, (int)threadIdx.x & 63, wave & 1);
     side.load(side.raw, h0);
-    side.load_common();
+    side.load_common(h0);
     const long long unit0 = kv_unit(p.cache, p.batch.table, p.batch.table_width, sequence, h0, w.blk);
     if (unit0 < 0) return;     // (all wavefronts)
     for (int h = h0; h < h1; ++h) {
@@ -311,6 +329,7 @@ __device__ __forceinline__ void append_heads(const KvAppendParams &p, const Bloc
         side.load_old(unit);
         Exchange &ex = exchange[h & 1];      // (written again two heads on: behind a barrier that every wavefront enters when it has read it)
         const uint32_t bad = side.look(), most = side.largest(bad);
+        side.load_next(h + 1 < h1 ? h + 1 : h);
         if (side.lane == 0) {
             ex.bad[wave] = bad;
             ex.top[wave] = most;
@@ -332,7 +351,7 @@ __device__ __forceinline__ void append_heads(const KvAppendParams &p, const Bloc
     }
 }
 
-template <int D>
+template <int D, bool NORM>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p, int heads_per_wg) {
     __shared__ Exchange exchange[2];
     const KvItem item = kv_item(p.batch, blockIdx.x, [&](int n, int value) {
@@ -349,7 +368,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p, int he
     w.row0 = (long long)item.first + (w.blk * kKvBlock - before);      // input row of the block's token 0 (rows lo .. hi - 1 are read)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h0 = blockIdx.y * heads_per_wg, h1 = h0 + heads_per_wg < p.cache.heads ? h0 + heads_per_wg : p.cache.heads;
-    if (wave < 2) append_heads<KeySide<D>>(p, w, item.sequence, h0, h1, p.cache.ks, wave, exchange);
+    if (wave < 2) append_heads<KeySide<D, NORM>>(p, w, item.sequence, h0, h1, p.cache.ks, wave, exchange);
     else append_heads<ValueSide<D>>(p, w, item.sequence, h0, h1, p.cache.vs, wave, exchange);
 }
 
@@ -437,12 +456,12 @@ hipError_t launch_kv_append(const KvAppendParams &p, hipStream_t stream) {
     const long long rounds = (long long)items * p.cache.heads / 1024;
     const int most = rounds < 1 ? 1 : rounds > 4 ? 4 : (int)rounds, per = most < p.cache.heads ? most : p.cache.heads;
     const dim3 grid(items, (p.cache.heads + per - 1) / per);
-    switch (p.cache.dim) {
-        case 64: kv_append_kernel<64><<<grid, 256, 0, stream>>>(p, per); break;
-        case 128: kv_append_kernel<128><<<grid, 256, 0, stream>>>(p, per); break;
-        case 256: kv_append_kernel<256><<<grid, 256, 0, stream>>>(p, per); break;
-        default: return hipErrorInvalidValue;
-    }
+    const auto kernel = p.cache.dim == 64    ? p.norm.on ? kv_append_kernel<64, true> : kv_append_kernel<64, false>
+                        : p.cache.dim == 128 ? p.norm.on ? kv_append_kernel<128, true> : kv_append_kernel<128, false>
+                        : p.cache.dim == 256 ? p.norm.on ? kv_append_kernel<256, true> : kv_append_kernel<256, false>
+                                             : nullptr;
+    if (!kernel) return hipErrorInvalidValue;
+    kernel<<<grid, 256, 0, stream>>>(p, per);
     return hipGetLastError();
 }
 

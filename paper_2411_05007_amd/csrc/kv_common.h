@@ -134,13 +134,49 @@ __device__ __forceinline__ void kv_load8(const float *p, float (&x)[8]) {
 __device__ __forceinline__ float kv_turn_a(float a, float b, float c, float s) { return a * c - b * s; }
 __device__ __forceinline__ float kv_turn_b(float a, float b, float c, float s) { return b * c + a * s; }
 
+// ---- norm of a head: y = x r w with r = 1 / sqrt(mean x^2 + eps), before the rotation ---------------------------------------------
+// Squares of numbers past 2^60 may leave fp32: rows whose sum does are taken 2^-72 times (eps is nothing beside them) and summed again, which happens in no ordinary call.
+constexpr float kKvTiny = 2.1175823681357508e-22f;      // 2^-72
+__device__ __forceinline__ float kv_norm_factor(float sum, float inv_dim, float eps) { return __builtin_amdgcn_rsqf(sum * inv_dim + eps); }      // within an ulp
+// weights of a token and head, null: ones
+__device__ __forceinline__ const float *kv_norm_row(const KvNorm &n, int pos, int head) {
+    const float *w = pos < n.first_tokens ? n.first : n.weight;
+    return w ? w + (size_t)head * n.head_stride : nullptr;
+}
+__device__ __forceinline__ void kv_load_weights(const float *row, int at, float (&w)[8]) {
+    if (row) {
+        kv_load8(row + at, w);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = 1.f;
+}
+__device__ __forceinline__ float kv_squares(float sum, const float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
+    return sum;
+}
+
 // Eight channels at each of N places of one row of 16-bit queries at position `pos`, rotated, in fp32; place(i) is a multiple of 8.  In the order of halves
 // the partners of eight neighbours are eight neighbours, in the interleaved order they are among themselves (dims is a multiple of 16).  Everything
-// is requested before the first is used; channels past `dims` are loaded like the others and left as they are.
-template <int N>
+// is requested before the first is used; channels past `dims` are loaded like the others and left as they are.  WEIGHTS: and normalised before, `ready` takes a run of
+// eight, and the weights for it.
+template <int N, bool WEIGHTS = false>
 struct KvRotating {
     uint4 own[N], other[N];
     float c[N][8], s[N][8];
+    float w[WEIGHTS ? N : 1][8], w_other[WEIGHTS ? N : 1][8];
+    // of the row's weights, null: ones
+    template <typename Place>
+    __device__ __forceinline__ void request_weights(const float *weights, const KvRope &rope, Place place) {
+        const int half = rope.dims / 2;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int d = place(i) < rope.dims ? place(i) : 0;
+            kv_load_weights(weights, place(i), w[WEIGHTS ? i : 0]);
+            if (rope.dims != 0 && !rope.interleaved) kv_load_weights(weights, d >= half ? d - half : d + half, w_other[WEIGHTS ? i : 0]);
+        }
+    }
     template <typename Place>
     __device__ __forceinline__ void request(const uint16_t *row, const KvRope &rope, int pos, Place place) {
 #pragma unroll
@@ -164,8 +200,15 @@ struct KvRotating {
     }
     template <typename Place>
     __device__ __forceinline__ void finish(const KvRope &rope, Place place, float (&x)[N][8]) const {
+        finish(rope, place, x, [](float (&)[8], const float (&)[8]) {});
+    }
+    template <typename Place, typename Ready>
+    __device__ __forceinline__ void finish(const KvRope &rope, Place place, float (&x)[N][8], Ready ready) const {
 #pragma unroll
-        for (int i = 0; i < N; ++i) kv_floats(own[i], x[i]);
+        for (int i = 0; i < N; ++i) {
+            kv_floats(own[i], x[i]);
+            ready(x[i], w[WEIGHTS ? i : 0]);
+        }
         if (rope.dims == 0) return;
         if (rope.interleaved) {
 #pragma unroll
@@ -185,6 +228,7 @@ struct KvRotating {
         for (int i = 0; i < N; ++i) {
             float y[8];
             kv_floats(other[i], y);
+            ready(y, w_other[WEIGHTS ? i : 0]);
             const bool turn = place(i) < rope.dims, second = place(i) >= half;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -225,6 +269,38 @@ __device__ __forceinline__ float kv_max_lanes(float x) {
     if (U >= 8) x = kv_max_dpp<0x141>(x);           // eight lanes backwards
     if (U >= 16) x = kv_max_dpp<0x140>(x);          // sixteen
     return x;
+}
+// sum over U = 4, 8 or 16 neighbouring lanes
+template <int CONTROL>
+__device__ __forceinline__ float kv_sum_dpp(float x) {
+    return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CONTROL, 0xf, 0xf, false));
+}
+template <int U>
+__device__ __forceinline__ float kv_sum_lanes(float x) {
+    x = kv_sum_dpp<0x4e>(kv_sum_dpp<0xb1>(x));
+    if (U >= 8) x = kv_sum_dpp<0x141>(x);
+    if (U >= 16) x = kv_sum_dpp<0x140>(x);
+    return x;
+}
+// A row of 16 U channels, sixteen of them in each of U neighbouring lanes (all lanes of the wavefront take part).
+template <int U>
+__device__ __forceinline__ void kv_normalise(float (&x)[2][8], const float (&w)[2][8], float eps) {
+    constexpr float kInverse = 1.f / (16 * U);
+    float sum = kv_sum_lanes<U>(kv_squares(kv_squares(0.f, x[0]), x[1]));
+    const bool large = !(sum < __builtin_inff());
+    if (__builtin_amdgcn_ballot_w64(large) != 0ull) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[j][e] = large ? x[j][e] * kKvTiny : x[j][e];
+        sum = kv_sum_lanes<U>(kv_squares(kv_squares(0.f, x[0]), x[1]));
+        eps = large ? 0.f : eps;
+    }
+    const float r = kv_norm_factor(sum, kInverse, eps);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[j][e] = x[j][e] * r * w[j][e];
 }
 __device__ __forceinline__ float kv_within_range(float x) { return __builtin_elementwise_maximum(__builtin_elementwise_minimum(x, 3.4028235e38f), -3.4028235e38f); }      // (NaN stays)
 // 1 / the sum of a row's weights, within an ulp (no key seen: zeros; NaN stays).  (The division proper is a chain of ten instructions, twice or three times a launch.)

@@ -45,7 +45,9 @@ constexpr int rows_lds_bytes(int D, int waves, int cap, int chunks) {
 }
 constexpr int kAgent = 16;      // cache policy of a buffer access that all XCDs see
 
-template <int D>
+// MORE: with a norm of the queries, or with first tokens that stay visible before a window (else the launch has neither).  Blocks count on without a gap then: first those of the
+// first tokens, then the window's, from v0 on; block_of() says which block of the sequence that is.
+template <int D, bool MORE>
 __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_rows_kernel(KvAttentionParams p) {
     constexpr int C = D / 32;                    // runs of 32 channels = steps of K Q^T per 16 tokens
     constexpr int kRow = row_floats(D);
@@ -71,12 +73,14 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     const int any_hi = hi_of(pos_z), all_hi = hi_of(pos_a);
     const int any_lo = p.causal && p.window > 0 && pos_a + 1 > p.window ? pos_a + 1 - p.window : 0, all_lo = p.causal && p.window > 0 && pos_z + 1 > p.window ? pos_z + 1 - p.window : 0;
     const int blk0 = any_lo >> 5, blk1 = (any_hi + 31) >> 5;
+    const int sinks = MORE ? p.sinks : 0, sink_blocks = (int)(((long long)sinks + 31) >> 5), v0 = MORE ? blk0 - (sink_blocks < blk0 ? sink_blocks : blk0) : blk0;
+    const auto block_of = [&](int v) { return MORE && v < blk0 ? v - v0 : v; };
     // this workgroup's blocks
-    const int chunk = blockIdx.x, count = blk1 > blk0 ? blk1 - blk0 : 0;
+    const int chunk = blockIdx.x, count = blk1 > blk0 ? blk1 - v0 : 0;
     int nchunks = (count + p.chunk_blocks - 1) / p.chunk_blocks;
     nchunks = nchunks < 1 ? 1 : nchunks > p.chunks ? p.chunks : nchunks;
     if (chunk >= nchunks) return;
-    const int c0 = blk0 + chunk * p.chunk_blocks, c1 = chunk == nchunks - 1 ? blk1 : c0 + p.chunk_blocks;
+    const int c0 = v0 + chunk * p.chunk_blocks, c1 = chunk == nchunks - 1 ? blk1 : c0 + p.chunk_blocks;
 
     const int32_t *table = p.batch.table + (size_t)b * p.batch.table_width;
     const int bs = p.cache.page_shift - 5;
@@ -84,10 +88,10 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     int base = c0 + wave, left = base < c1 ? (c1 - base + WAVES - 1) / WAVES : 0, here = 0, page_l = -1, kb_l = 0, vb_l = 0;
     auto look_up = [&]() {
         here = left < 64 ? left : 64;
-        page_l = here == 0 ? -1 : table[(base + WAVES * (lane < here ? lane : 0)) >> bs];
+        page_l = here == 0 ? -1 : table[block_of(base + WAVES * (lane < here ? lane : 0)) >> bs];
     };
     auto look_up_bytes = [&]() {
-        const int blk = base + WAVES * lane;
+        const int blk = block_of(base + WAVES * lane);
         const bool named = lane < here && (uint32_t)page_l < (uint32_t)p.cache.pages;
         const size_t u = named ? (((size_t)page_l * p.cache.heads + head) << bs) + (blk & ((1 << bs) - 1)) : 0;
         page_l = named ? page_l : -1;
@@ -100,7 +104,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     auto load = [&](Block<D> &t, int i) {
         const int page = __builtin_amdgcn_readlane(page_l, i < here ? i : 0);
         const bool real = i < here && page >= 0;
-        const size_t u = real ? (((size_t)page * p.cache.heads + head) << bs) + ((base + WAVES * i) & ((1 << bs) - 1)) : 0;
+        const size_t u = real ? (((size_t)page * p.cache.heads + head) << bs) + (block_of(base + WAVES * i) & ((1 << bs) - 1)) : 0;
         const uint8_t *k = p.cache.k + u * (32 * D), *v = p.cache.v + u * (32 * D);
         const uint32_t ko = real ? k_off : 0u, vo = real ? v_off : 0u;
 #pragma unroll
@@ -117,8 +121,15 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
         const int c = wave * kMine + i < C ? wave * kMine + i : C - 1;
         return 64 * (c / 2) + 16 * q4 + 8 * (c % 2);
     };
-    KvRotating<kMine> turning;
-    turning.request(p.q.data + (size_t)(t0 + tok) * p.q.token_stride + qh * p.q.head_stride, p.rope, pos, place);
+    KvRotating<kMine, MORE> turning;
+    const uint16_t *row = p.q.data + (size_t)(t0 + tok) * p.q.token_stride + qh * p.q.head_stride;
+    turning.request(row, p.rope, pos, place);
+    uint4 whole[MORE ? C : 1];      // the row's other channels too, for the mean of its squares
+    if (MORE && p.norm.on) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) whole[MORE ? c : 0] = *reinterpret_cast<const uint4 *>(row + 64 * (c / 2) + 16 * q4 + 8 * (c % 2));
+        turning.request_weights(kv_norm_row(p.norm, pos, qh), p.rope, place);
+    }
     __builtin_amdgcn_sched_barrier(0);
     look_up_bytes();
     Block<D> even, odd;
@@ -130,7 +141,34 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     float to_t;      // score -> exponent of 2, but for the block's scale
     {
         float x[kMine][8];
-        turning.finish(p.rope, place, x);
+        if (MORE && p.norm.on) {
+            const auto squares = [&](float by) {
+                float sum = 0.f;
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    float y[8];
+                    kv_floats(whole[MORE ? c : 0], y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] *= by;
+                    sum = kv_squares(sum, y);
+                }
+                return kv_sum32(kv_sum16(sum));
+            };
+            float sum = squares(1.f), by = 1.f, eps = p.norm.eps;
+            const bool large = !(sum < __builtin_inff());
+            if (__builtin_amdgcn_ballot_w64(large) != 0ull) {
+                by = large ? kKvTiny : 1.f;
+                eps = large ? 0.f : eps;
+                sum = squares(by);
+            }
+            const float factor = kv_norm_factor(sum, 1.f / D, eps);
+            turning.finish(p.rope, place, x, [&](float (&y)[8], const float (&w)[8]) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = y[e] * by * factor * w[e];
+            });
+        } else {
+            turning.finish(p.rope, place, x);
+        }
         uint32_t top = 0u;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
@@ -171,7 +209,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
 
     // exponents t of block i's weights, -inf where the row does not see the token; values of tokens that do not exist are cleared
     auto scores = [&](Block<D> &cur, int i, float (&t)[8]) {
-        const int blk = base + WAVES * i, kb = __builtin_amdgcn_readlane(kb_l, i);
+        const int blk = block_of(base + WAVES * i), kb = __builtin_amdgcn_readlane(kb_l, i);
         const bool named = __builtin_amdgcn_readlane(page_l, i) >= 0;
         kv_floatx4 s[2] = {};
 #pragma unroll
@@ -191,7 +229,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int key = first + (j & 3) + 8 * (j >> 2);
-                const bool ok = named && key >= seen_lo && key < seen_hi && key < len;
+                const bool ok = named && (key >= seen_lo || (MORE && key < sinks)) && key < seen_hi && key < len;
                 t[j] = ok ? t[j] : -__builtin_inff();
                 if (!named || key >= len) live[j >> 2] &= ~(0xffu << (8 * (j & 3)));
             }
@@ -437,26 +475,27 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     for (int i = threadIdx.x; i < nchunks; i += WAVES * 64) __hip_atomic_store(words + i, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <int D>
+template <int D, bool MORE>
 hipError_t launch_rows(const KvAttentionParams &p, hipStream_t stream) {
     static LdsLimit limit;
     constexpr int most = rows_lds_bytes(D, WAVES, 16, kKvMostChunks);
     if (p.chunks > kKvMostChunks) return hipErrorInvalidValue;
     if (most > 65536) {
-        const hipError_t e = limit.raise(reinterpret_cast<const void *>(kv_rows_kernel<D>), most);
+        const hipError_t e = limit.raise(reinterpret_cast<const void *>(kv_rows_kernel<D, MORE>), most);
         if (e != hipSuccess) return e;
     }
-    kv_rows_kernel<D><<<dim3(p.chunks, p.cache.heads, p.batch.sequences * p.row_tiles), WAVES * 64, rows_lds_bytes(D, WAVES, p.row_cap, p.chunks), stream>>>(p);
+    kv_rows_kernel<D, MORE><<<dim3(p.chunks, p.cache.heads, p.batch.sequences * p.row_tiles), WAVES * 64, rows_lds_bytes(D, WAVES, p.row_cap, p.chunks), stream>>>(p);
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_kv_attention_rows(const KvAttentionParams &p, hipStream_t stream) {
+    const bool more = p.norm.on || p.sinks > 0;
     switch (p.cache.dim) {
-        case 64: return launch_rows<64>(p, stream);
-        case 128: return launch_rows<128>(p, stream);
-        case 256: return launch_rows<256>(p, stream);
+        case 64: return more ? launch_rows<64, true>(p, stream) : launch_rows<64, false>(p, stream);
+        case 128: return more ? launch_rows<128, true>(p, stream) : launch_rows<128, false>(p, stream);
+        case 256: return more ? launch_rows<256, true>(p, stream) : launch_rows<256, false>(p, stream);
         default: return hipErrorInvalidValue;
     }
 }

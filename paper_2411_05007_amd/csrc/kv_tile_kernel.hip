@@ -44,7 +44,9 @@ constexpr int tile_lds_bytes(int D, int waves) {
     return tiles > queries ? tiles > out ? tiles : out : queries > out ? queries : out;
 }
 
-template <int D, int WAVES>
+// MORE: with a norm of the queries, or with first tokens that stay visible before a window (else the launch has neither).  Tiles count on without a gap then: first those of the
+// first tokens, then the window's; key_of() and block_of() say where in the sequence that is.
+template <int D, int WAVES, bool MORE>
 __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(KvAttentionParams p) {
     constexpr int C = D / 16, A = D / 32, kRows = 32 * WAVES, kThreads = 64 * WAVES;
     constexpr int N = kTileKeys * D / (kThreads * 16);      // 16-byte pieces of a tile of codes per thread: 1, 2, 4
@@ -66,7 +68,11 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     const int all_lo = lo_of(w_last), all_hi = hi_of(w_first);
     const bool idle = row0 + wave * 32 >= rows;      // no row is left for the wavefront: it brings codes to LDS, and leaves its SIMD to the others
     // tiles of keys, and this part's share of them
-    const int key_a = wg_lo / kTileKeys * kTileKeys, tiles_a = wg_hi > key_a ? (wg_hi - key_a + kTileKeys - 1) / kTileKeys : 0;
+    const int window_a = wg_lo / kTileKeys * kTileKeys;      // the window's first tile
+    const int sinks = MORE ? p.sinks : 0, sink_keys = (int)(((long long)sinks + kTileKeys - 1) / kTileKeys * kTileKeys), gap = MORE ? window_a - (sink_keys < window_a ? sink_keys : window_a) : 0;
+    const auto key_of = [&](int key) { return MORE && key < window_a ? key - gap : key; };
+    const auto block_of = [&](int blk) { return MORE && blk < window_a >> 5 ? blk - (gap >> 5) : blk; };
+    const int key_a = MORE ? gap : window_a, tiles_a = wg_hi > window_a ? (wg_hi - key_a + kTileKeys - 1) / kTileKeys : 0;
     const int tile0 = (int)((long long)tiles_a * part / p.parts), tiles_k = (int)((long long)tiles_a * (part + 1) / p.parts) - tile0;
     const int key0 = key_a + tile0 * kTileKeys;
 
@@ -79,11 +85,11 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     bool wide = false;      // the values' scales are too far apart for one reference (the same in all wavefronts)
     auto look_up_pages = [&](int t) {      // t a multiple of 32
         const int blk = blk0 + 2 * t + lane;
-        unit_a = blk < blk1 ? table[blk >> bs] : -1;
+        unit_a = blk < blk1 ? table[block_of(blk) >> bs] : -1;
     };
     auto look_up_bytes = [&](int t) {
         const bool named = (uint32_t)unit_a < (uint32_t)p.cache.pages;
-        unit_a = named ? (int)((((uint32_t)unit_a * (uint32_t)p.cache.heads + (uint32_t)head) << bs) + ((blk0 + 2 * t + lane) & ((1 << bs) - 1))) : -1;
+        unit_a = named ? (int)((((uint32_t)unit_a * (uint32_t)p.cache.heads + (uint32_t)head) << bs) + (block_of(blk0 + 2 * t + lane) & ((1 << bs) - 1))) : -1;
         const size_t u = named ? (size_t)(uint32_t)unit_a : 0;
         kb_a = p.cache.ks[u];
         vb_a = p.cache.vs[u];
@@ -131,7 +137,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         if (decltype(partial)::value) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (key0 + t * kTileKeys + 32 * blk + kv_slot_token(g) + (j & 3) + 8 * (j >> 2) >= len) live[j >> 2] &= ~(0xffu << (8 * (j & 3)));
+                if (key_of(key0 + t * kTileKeys) + 32 * blk + kv_slot_token(g) + (j & 3) + 8 * (j >> 2) >= len) live[j >> 2] &= ~(0xffu << (8 * (j & 3)));
         }
         unsigned char *dst = vt + ((blk * A + a) * 4 + g) * kSlotBytes + d16 * 16;
         *reinterpret_cast<kv_f16x8 *>(dst) = kv_f16_of(w[i].x & live[0], w[i].y & live[1], vf);
@@ -151,7 +157,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     // LDS as operands. ----
     kv_f16x8 qf[C];
     float to_t = 0.f;      // score -> exponent of 2, but for the block's scale; not negative: a negative scale turns the queries' sign
-    constexpr int U = D / 16, PER = U < 8 ? U / 2 : 4;      // units of a row, of a lane at a time
+    constexpr int U = D / 16, PER = U < 8 || MORE ? 2 : 4;      // units of a row, of a lane at a time (with weights of a norm beside them: fewer)
     constexpr int kChunk = 33 * 16;         // bytes of a run of eight channels of 32 rows in LDS
     unsigned char *my_queries = lds + wave * (2 * U * kChunk + 128);
     float *factors = reinterpret_cast<float *>(my_queries + 2 * U * kChunk);
@@ -190,6 +196,14 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
                 float x[2][8];
                 kv_floats(own[i][0], x[0]);
                 kv_floats(own[i][1], x[1]);
+                if (MORE && p.norm.on) {
+                    const int r = row0 + wave * 32 + row < rows ? row0 + wave * 32 + row : rows - 1;
+                    const float *weights = kv_norm_row(p.norm, len - n + r / p.group, head * p.group + r % p.group);
+                    float w[2][8];
+                    kv_load_weights(weights, halves ? pr * 8 : pr * 16, w[0]);
+                    kv_load_weights(weights, halves ? pr * 8 + half : pr * 16 + 8, w[1]);
+                    kv_normalise<U>(x, w, p.norm.eps);
+                }
                 const float cc[8] = {c[i][0].x, c[i][0].y, c[i][0].z, c[i][0].w, c[i][1].x, c[i][1].y, c[i][1].z, c[i][1].w};
                 const float ss[8] = {s[i][0].x, s[i][0].y, s[i][0].z, s[i][0].w, s[i][1].x, s[i][1].y, s[i][1].z, s[i][1].w};
                 if (turn) {
@@ -271,7 +285,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     };
     // masks the scores of tile t and renews the maximum if they pass it; top: largest(s)
     auto look_at = [&](Scores &s, float (&top)[2], const Facts &f, int t) {
-        const int key = key0 + t * kTileKeys;
+        const int key = key_of(key0 + t * kTileKeys);
         if (!named(f) || key < all_lo || key + kTileKeys > all_hi) {
             const int pos = pos_of(row0 + wave * 32 + l32), seen_hi = hi_of(pos) < len ? hi_of(pos) : len, seen_lo = lo_of(pos);
 #pragma unroll
@@ -279,7 +293,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int at = key + 32 * i + 8 * (v >> 2) + 4 * h32 + (v & 3);
-                    s[i][v] = f.unit[i] != -1 && at >= seen_lo && at < seen_hi ? s[i][v] : -__builtin_inff();
+                    s[i][v] = f.unit[i] != -1 && (at >= seen_lo || (MORE && at < sinks)) && at < seen_hi ? s[i][v] : -__builtin_inff();
                 }
             largest(s, top);
         }
@@ -474,7 +488,8 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         l = 0.f;
         row_ref = 0;
         const int pos = pos_of(row0 + wave * 32 + l32), seen_hi = hi_of(pos) < len ? hi_of(pos) : len, seen_lo = lo_of(pos);
-        for (int blk = blk0; blk < blk1; ++blk) {
+        for (int v_blk = blk0; v_blk < blk1; ++v_blk) {
+            const int blk = block_of(v_blk);
             const long long unit = kv_unit(p.cache, p.batch.table, p.batch.table_width, b, head, blk);
             if (unit < 0) continue;
             const uint8_t *k = p.cache.k + (size_t)unit * (32 * D) + l32 * D + 8 * h32, *v = p.cache.v + (size_t)unit * (32 * D) + (l32 % 16 * 4 + h32) * 16 + l32 / 16 * 8;
@@ -489,7 +504,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int at = blk * kKvBlock + 8 * (i >> 2) + 4 * h32 + (i & 3);
-                s[i] = at >= seen_lo && at < seen_hi ? s[i] * f : -__builtin_inff();
+                s[i] = (at >= seen_lo || (MORE && at < sinks)) && at < seen_hi ? s[i] * f : -__builtin_inff();
                 top = fmaxf(top, s[i]);
             }
             top = kv_max32(top);
@@ -600,22 +615,27 @@ __global__ __launch_bounds__(256) void kv_meet_kernel(KvAttentionParams p) {
     *reinterpret_cast<uint2 *>(p.out + row * D + d) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
 }
 
-template <int D, int WAVES>
-hipError_t launch_tile(const KvAttentionParams &p, hipStream_t stream) {
+template <int D, int WAVES, bool MORE>
+hipError_t launch_tile_of(const KvAttentionParams &p, hipStream_t stream) {
     static LdsLimit limit;
     constexpr int bytes = tile_lds_bytes(D, WAVES);
     if (bytes > 65536) {
-        const hipError_t e = limit.raise(reinterpret_cast<const void *>(kv_tile_kernel<D, WAVES>), bytes);
+        const hipError_t e = limit.raise(reinterpret_cast<const void *>(kv_tile_kernel<D, WAVES, MORE>), bytes);
         if (e != hipSuccess) return e;
     }
     const long long items = (long long)p.batch.total * p.group / (32 * WAVES) + p.batch.sequences;
-    kv_tile_kernel<D, WAVES><<<dim3((uint32_t)(items * p.cache.heads), p.parts), 64 * WAVES, bytes, stream>>>(p);
+    kv_tile_kernel<D, WAVES, MORE><<<dim3((uint32_t)(items * p.cache.heads), p.parts), 64 * WAVES, bytes, stream>>>(p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
     const size_t rows = (size_t)p.batch.total * p.q_heads;
     constexpr int per = 256 / (D / 4);
     kv_meet_kernel<D><<<(uint32_t)((rows + per - 1) / per), 256, 0, stream>>>(p);
     return hipGetLastError();
+}
+
+template <int D, int WAVES>
+hipError_t launch_tile(const KvAttentionParams &p, hipStream_t stream) {
+    return p.norm.on || p.sinks > 0 ? launch_tile_of<D, WAVES, true>(p, stream) : launch_tile_of<D, WAVES, false>(p, stream);
 }
 
 }  // namespace

@@ -49,6 +49,24 @@ class Rope:
         self.cdesc = S.KVRopeDev(table.data_ptr(), table.shape[0], table.shape[1], int(self.interleaved))
 
 
+class KVNorm:
+    """Norm of queries and keys for each head, before the rotation: w x / sqrt(mean x^2 + eps).  q, k: fp32 weights on the GPU, [head_dim] or [heads, head_dim] (both alike);
+    None: ones.  Tokens at positions below first_tokens take q_first and k_first."""
+
+    def __init__(self, q=None, k=None, eps: float = 1e-6, q_first=None, k_first=None, first_tokens: int = 0):
+        self.q, self.k, self.q_first, self.k_first, self.eps = q, k, q_first, k_first, float(eps)
+        given = [t for t in (q, k, q_first, k_first) if t is not None]
+        for t in given:
+            assert t.dtype is torch.float32 and t.is_cuda and t.is_contiguous() and t.dim() in (1, 2), "weights: contiguous fp32 [head_dim] or [heads, head_dim] on the GPU"
+        assert len({t.dim() for t in given}) <= 1, "weights: all for each head, or none"
+        at = lambda t: None if t is None else t.data_ptr()
+        self.cdesc = S.KVNormDev(at(q), at(k), at(q_first), at(k_first), int(first_tokens), int(bool(given) and given[0].dim() == 2), self.eps)
+
+    def _check(self, name: str, heads: int, dim: int) -> None:
+        for t in (getattr(self, name), getattr(self, name + "_first")):
+            assert t is None or tuple(t.shape) == ((heads, dim) if t.dim() == 2 else (dim,)), f"norm: weights of {tuple(t.shape)} for {heads} heads of {dim}"
+
+
 class KVBatch:
     """New tokens of some sequences.  cu_new int32 [B + 1], kv_len int32 [B] (tokens with the new ones), block_table int32 [B, width], all on the GPU;
     new_tokens = cu_new[B]; no sequence has more than max_new new tokens or more than max_len tokens."""
@@ -128,10 +146,13 @@ class KVCache:
             t.record_stream(current)
         return t
 
-    def append(self, k, v, batch: KVBatch, rope: Optional[Rope] = None, stream=None) -> None:
+    def append(self, k, v, batch: KVBatch, rope: Optional[Rope] = None, stream=None, norm: Optional[KVNorm] = None) -> None:
         """k, v: bf16 [new_tokens, kv_heads, head_dim] (any token and head stride that keeps 16-byte alignment)."""
         kd, vd = self._rows(k, self.kv_heads, batch.new_tokens, "k"), self._rows(v, self.kv_heads, batch.new_tokens, "v")
-        S._check(S.lib().svdq_kv_append(self.cdesc, batch.cdesc, None if rope is None else rope.cdesc, kd, vd, self._stream(stream)), "svdq_kv_append")
+        if norm is not None:
+            norm._check("k", self.kv_heads, self.head_dim)
+        S._check(S.lib().svdq_kv_append_normed(self.cdesc, batch.cdesc, None if norm is None else norm.cdesc, None if rope is None else rope.cdesc, kd, vd,
+                                               self._stream(stream)), "svdq_kv_append")
 
     def attention_workspace(self, batch: KVBatch, q_heads: int, stream=None):
         n = S.lib().svdq_kv_attention_workspace_bytes(C.byref(self.shape), int(q_heads), batch.sequences, batch.max_new, batch.max_len)
@@ -140,8 +161,9 @@ class KVCache:
         return self._new(n, torch.uint8, stream)
 
     def attention(self, q, batch: KVBatch, rope: Optional[Rope] = None, scale: Optional[float] = None, causal: bool = True, window: int = 0,
-                  out=None, workspace=None, stream=None):
-        """q: bf16 [new_tokens, q_heads, head_dim].  Returns bf16 of the same shape, contiguous.  scale: 1 / sqrt(head_dim) if None."""
+                  out=None, workspace=None, stream=None, norm: Optional[KVNorm] = None, sinks: int = 0):
+        """q: bf16 [new_tokens, q_heads, head_dim].  Returns bf16 of the same shape, contiguous.  scale: 1 / sqrt(head_dim) if None.  window: how many of the last tokens a
+        row sees (0: all), sinks: first tokens of a sequence that it sees beside them."""
         qd = self._rows(q, None, batch.new_tokens, "q")
         heads = q.shape[1]
         if out is None:
@@ -152,9 +174,11 @@ class KVCache:
             workspace = self.attention_workspace(batch, heads, stream)
         else:
             assert workspace.dtype is torch.uint8 and workspace.is_cuda and workspace.is_contiguous(), "workspace: uint8 on the GPU"
-        S._check(S.lib().svdq_kv_attention(self.cdesc, batch.cdesc, None if rope is None else rope.cdesc, qd, heads,
-                                           1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(causal), int(window), out.data_ptr(),
-                                           workspace.data_ptr(), workspace.numel(), self._stream(stream)), "svdq_kv_attention")
+        if norm is not None:
+            norm._check("q", heads, self.head_dim)
+        S._check(S.lib().svdq_kv_attention_normed(self.cdesc, batch.cdesc, None if norm is None else norm.cdesc, None if rope is None else rope.cdesc, qd, heads,
+                                                  1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(causal), int(window), int(sinks), out.data_ptr(),
+                                                  workspace.data_ptr(), workspace.numel(), self._stream(stream)), "svdq_kv_attention")
         return out
 
     def gather(self, rows: KVRows, out=None, stream=None):

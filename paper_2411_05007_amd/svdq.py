@@ -32,6 +32,7 @@ EXPORTS = [
     "svdq_forward_options", "svdq_profile_event", "svdq_mfma_peak_probe", "svdq_linear_forward_static",
     "svdq_debug_launch_plan",
     "svdq_kv_cache_sizes", "svdq_kv_append", "svdq_kv_attention_workspace_bytes", "svdq_kv_attention", "svdq_kv_gather",
+    "svdq_kv_append_normed", "svdq_kv_attention_normed",
 ]
 
 
@@ -69,6 +70,10 @@ class KVBatchDev(C.Structure):
 
 class KVRopeDev(C.Structure):
     _fields_ = [("table", C.c_void_p), ("positions", C.c_int), ("dims", C.c_int), ("interleaved", C.c_int)]
+
+
+class KVNormDev(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_weight", "k_weight", "q_first", "k_first")] + [("first_tokens", C.c_int), ("per_head", C.c_int), ("eps", C.c_float)]
 
 
 class KVRowsDev(C.Structure):
@@ -135,6 +140,9 @@ def lib() -> C.CDLL:
         L.svdq_kv_attention_workspace_bytes.argtypes = [C.POINTER(KVShape)] + [C.c_int] * 4
         L.svdq_kv_attention.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), C.POINTER(KVRopeDev), C.POINTER(KVRowsDev), C.c_int, C.c_float, C.c_int, C.c_int,
                                         vp, vp, C.c_size_t, vp]
+        L.svdq_kv_append_normed.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), C.POINTER(KVNormDev), C.POINTER(KVRopeDev), C.POINTER(KVRowsDev), C.POINTER(KVRowsDev), vp]
+        L.svdq_kv_attention_normed.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), C.POINTER(KVNormDev), C.POINTER(KVRopeDev), C.POINTER(KVRowsDev), C.c_int, C.c_float,
+                                               C.c_int, C.c_int, C.c_int, vp, vp, C.c_size_t, vp]
         L.svdq_kv_gather.argtypes = [C.POINTER(KVCacheDev), vp, vp, vp, C.c_int, C.c_int, C.c_int, vp, vp, vp]
         _lib = L
     return _lib
