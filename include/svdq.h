@@ -477,6 +477,26 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
                              size_t workspace_bytes, void *hip_stream);
 
 /*
+ * Compaction: some of a sequence's tokens become its tokens from to_first[b] on, in the order in which they are given: token to_first[b] + i is what token
+ * from_token[cu_moves[b] + i] was (with per_head: from_token[head][moves], a list for each head).  Any choice and order will do, a token may be taken twice.  Pages are those of
+ * from_table for what is read, in the cache `from`, and of to_table for what is written, in `to` (the same cache or another one, of as many heads and the same head_dim).
+ * With a rope, keys are turned from the position that the token had to the one that it gets (the table that they were appended with; its rows need not have size one); a token
+ * that keeps its position keeps its key.  Blocks are quantized as by an append of the moved vectors in that order: tokens before to_first[b] in its block stay, at the larger
+ * byte; what lies behind the last move in its block is lost.  A token that no page of from_table holds becomes one with NaN codes, as do those that have some.
+ *   workspace NULL: no page that is written is one that is read.  Otherwise (256-byte aligned, >= svdq_kv_compact_workspace_bytes(), no initial contents) pages may be read and
+ *   written in the same call, as where a sequence shrinks in place; no page is written for two sequences.
+ * One kernel, a second one with a workspace.  SVDQ_EINVAL and SVDQ_EUNSUPPORTED as above, SVDQ_EINVAL also for caches that do not fit each other.
+ */
+typedef struct {
+    const int32_t *cu_moves, *from_token, *to_first; /* device: [sequences + 1], [moves] or [kv_heads][moves], [sequences] */
+    const int32_t *from_table, *to_table;            /* device: [sequences][from_width], [sequences][to_width] */
+    int sequences, from_width, to_width, moves, per_head;
+} svdq_kv_moves;
+size_t svdq_kv_compact_workspace_bytes(const svdq_kv_shape *shape, int sequences, int moves);
+int svdq_kv_compact(const svdq_kv_cache_dev *to, const svdq_kv_cache_dev *from, const svdq_kv_moves *moves, const svdq_kv_rope *rope,
+                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Rows of the cache as bf16 [rows][kv_heads][head_dim] (16-byte aligned; either output may be NULL): sequence b's tokens first_token[b] ..
  * onwards are rows cu_rows[b] .. cu_rows[b + 1] - 1.  Exact where code * scale is a normal bf16.  Zeros where the table names no page.
  */

@@ -91,3 +91,25 @@ def attention(q, size, k, v, positions, keys, scale, causal=True, window=0, sink
         out[bad, h] = np.nan
     return out, tol
 
+
+
+def moved_key(k, old, new, table, interleaved):
+    """Keys fp64 [n, heads, D] turned from positions old ([n] or [n, heads]) to new [n].  Returns them and what fp32 may be off by: with u = 2^-24, cosines and sines of the
+    difference come of three products and sums and a division by a reciprocal of 1 ulp (under 12 u of |c1 c0| + |s1 s0| over c0^2 + s0^2, which is at most
+    the ratio g of the sizes of the two entries), the turning adds two products and a sum (3 u): (12 + 3) u g (|a| + |b|) < 2^-20 g (|a| + |b|); a code times its scale is exact."""
+    back, _ = turn(k, old, table, interleaved, back=True)
+    out, _ = turn(back, new, table, interleaved)
+    stays = np.asarray(old) == (np.asarray(new) if np.ndim(old) == 1 else np.asarray(new)[:, None])
+    stays = stays[:, None, None] if np.ndim(old) == 1 else stays[..., None]
+    out = np.where(stays, k, out)
+    slack = np.zeros_like(k)
+    if table is not None:
+        dims = table.shape[1]
+        i, j = (np.arange(0, dims, 2), np.arange(1, dims, 2)) if interleaved else (np.arange(dims // 2), np.arange(dims // 2, dims))
+        t = np.asarray(table, np.float64)
+        size = lambda p: np.sqrt(t[np.minimum(p, len(t) - 1), :dims // 2] ** 2 + t[np.minimum(p, len(t) - 1), dims // 2:] ** 2)
+        lift = lambda z: z[:, None] if z.ndim == 2 else z
+        g = lift(size(np.asarray(new))) / lift(size(np.asarray(old)))
+        both = 2.0 ** -20 * g * (np.abs(k[..., i]) + np.abs(k[..., j]))
+        slack[..., i], slack[..., j] = both, both
+    return out, np.where(stays, 0.0, slack)

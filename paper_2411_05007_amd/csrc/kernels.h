@@ -236,6 +236,17 @@ struct KvAppendParams {
     KvNorm norm;             // of the keys
 };
 hipError_t launch_kv_append(const KvAppendParams &p, hipStream_t stream);
+struct KvCompactParams {
+    KvCache to, from;        // of the same heads and dim
+    KvBatch batch;           // cu: a sequence's moves; kv_len: the token that its first move becomes; table, total: of `to`, moves in all
+    const int32_t *from_token;       // [moves], or [heads][moves]: the token that it was
+    const int32_t *from_table;       // [sequences][from_width]
+    int from_width, per_head;
+    KvRope rope;             // of the keys: from the old position to the new one
+    uint8_t *stage;          // null, or [item][head] blocks: 32 dim codes of keys, of values
+    uint8_t *stage_bytes;    // [item][head][2]
+};
+hipError_t launch_kv_compact(const KvCompactParams &p, hipStream_t stream);
 struct KvGatherParams {
     KvCache cache;
     KvBatch batch;

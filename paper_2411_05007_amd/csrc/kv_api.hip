@@ -174,6 +174,40 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
     return done(svdq::launch_kv_attention_rows(p, stream));
 }
 
+size_t svdq_kv_compact_workspace_bytes(const svdq_kv_shape *shape, int sequences, int moves) {
+    if (!shape || check_shape(*shape) != SVDQ_OK || sequences < 0 || moves < 0) return 0;
+    const size_t blocks = ((size_t)moves / 32 + 2 * (size_t)sequences) * shape->kv_heads;
+    return blocks == 0 ? 256 : blocks * 64 * shape->head_dim + (2 * blocks + 255) / 256 * 256;
+}
+
+int svdq_kv_compact(const svdq_kv_cache_dev *to, const svdq_kv_cache_dev *from, const svdq_kv_moves *moves, const svdq_kv_rope *rope, void *workspace,
+                    size_t workspace_bytes, void *hip_stream) {
+    int st = check_cache(to);
+    if (st != SVDQ_OK || (st = check_cache(from)) != SVDQ_OK) return st;
+    if (!moves || to->shape.kv_heads != from->shape.kv_heads || to->shape.head_dim != from->shape.head_dim) return SVDQ_EINVAL;
+    if ((st = check_tables(moves->cu_moves, moves->to_first, moves->to_table, moves->sequences, moves->to_width, moves->moves, to->shape.page_tokens)) != SVDQ_OK) return st;
+    if ((st = check_tables(moves->cu_moves, moves->from_token, moves->from_table, moves->sequences, moves->from_width, moves->moves, from->shape.page_tokens)) != SVDQ_OK) return st;
+    if ((st = check_rope(rope, to->shape.head_dim)) != SVDQ_OK) return st;
+    if (moves->sequences > kMaxGridY) return SVDQ_EUNSUPPORTED;
+    if (workspace) {
+        if ((uintptr_t)workspace & 255) return SVDQ_EINVAL;
+        if (workspace_bytes < svdq_kv_compact_workspace_bytes(&to->shape, moves->sequences, moves->moves)) return SVDQ_ENOSPACE;
+    }
+    if (moves->sequences == 0 || moves->moves == 0) return SVDQ_OK;
+    svdq::KvCompactParams p{};
+    p.to = cache_of(to);
+    p.from = cache_of(from);
+    p.batch = svdq::KvBatch{moves->cu_moves, moves->to_first, moves->to_table, moves->sequences, moves->to_width, moves->moves};
+    p.from_token = moves->from_token;
+    p.from_table = moves->from_table;
+    p.from_width = moves->from_width;
+    p.per_head = moves->per_head != 0;
+    p.rope = rope_of(rope);
+    p.stage = static_cast<uint8_t *>(workspace);
+    if (workspace) p.stage_bytes = p.stage + ((size_t)moves->moves / 32 + 2 * (size_t)moves->sequences) * to->shape.kv_heads * 64 * to->shape.head_dim;
+    return done(svdq::launch_kv_compact(p, static_cast<hipStream_t>(hip_stream)));
+}
+
 int svdq_kv_gather(const svdq_kv_cache_dev *cache, const int32_t *first_token, const int32_t *cu_rows, const int32_t *block_table, int sequences,
                    int table_width, int rows, void *out_k, void *out_v, void *hip_stream) {
     int st = check_cache(cache);

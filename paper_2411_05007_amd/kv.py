@@ -93,6 +93,22 @@ class KVRows:
         self.pointers, self.width = (first_token.data_ptr(), cu_rows.data_ptr(), block_table.data_ptr()), block_table.shape[1]
 
 
+class KVMoves:
+    """Tokens that become a sequence's tokens from to_first[b] on: those of numbers from_token[cu_moves[b]] .. from_token[cu_moves[b + 1] - 1], in that order.  All int32 on the
+    GPU: cu_moves [B + 1], from_token [moves] or [1, moves], or [kv_heads, moves] for lists of each head's own, to_first [B], from_table and to_table [B, width]."""
+
+    def __init__(self, cu_moves, from_token, to_first, from_table, to_table, moves: int):
+        for t, n in ((cu_moves, "cu_moves"), (from_token, "from_token"), (to_first, "to_first"), (from_table, "from_table"), (to_table, "to_table")):
+            _device_int32(t, n)
+        B = to_first.shape[0]
+        assert cu_moves.shape == (B + 1,) and from_table.dim() == 2 and to_table.dim() == 2 and from_table.shape[0] == to_table.shape[0] == B
+        assert from_token.dim() in (1, 2) and from_token.shape[-1] == moves, "from_token: [moves] or [heads, moves]"
+        self.cu_moves, self.from_token, self.to_first, self.from_table, self.to_table, self.sequences, self.moves = cu_moves, from_token, to_first, from_table, to_table, B, int(moves)
+        self.lists = 1 if from_token.dim() == 1 else from_token.shape[0]
+        self.cdesc = S.KVMovesDev(cu_moves.data_ptr(), from_token.data_ptr(), to_first.data_ptr(), from_table.data_ptr(), to_table.data_ptr(), B, from_table.shape[1],
+                                  to_table.shape[1], self.moves, int(self.lists > 1))
+
+
 class KVCache:
     """Pages of E4M3 codes with a scale byte for each 32 tokens and head, resident in HBM."""
 
@@ -180,6 +196,20 @@ class KVCache:
                                                   1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(causal), int(window), int(sinks), out.data_ptr(),
                                                   workspace.data_ptr(), workspace.numel(), self._stream(stream)), "svdq_kv_attention")
         return out
+
+    def compact_workspace(self, moves: KVMoves, stream=None):
+        n = S.lib().svdq_kv_compact_workspace_bytes(C.byref(self.shape), moves.sequences, moves.moves)
+        if n == 0:
+            raise S.SvdqError("unsupported shape")
+        return self._new(n, torch.uint8, stream)
+
+    def compact(self, moves: KVMoves, rope: Optional[Rope] = None, source: Optional["KVCache"] = None, workspace=None, stream=None) -> None:
+        """Moves tokens into pages of this cache, out of pages of `source` (None: of this cache).  rope: turns their keys to the new positions.  workspace (compact_workspace()):
+        needed where pages that are written are read as well."""
+        assert moves.lists in (1, self.kv_heads), f"from_token: {moves.lists} lists for {self.kv_heads} heads"
+        assert workspace is None or (workspace.dtype is torch.uint8 and workspace.is_cuda and workspace.is_contiguous()), "workspace: uint8 on the GPU"
+        at, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        S._check(S.lib().svdq_kv_compact(self.cdesc, (source or self).cdesc, moves.cdesc, None if rope is None else rope.cdesc, at, size, self._stream(stream)), "svdq_kv_compact")
 
     def gather(self, rows: KVRows, out=None, stream=None):
         """Keys and values bf16 [rows, kv_heads, head_dim] as they are held."""

@@ -32,7 +32,7 @@ EXPORTS = [
     "svdq_forward_options", "svdq_profile_event", "svdq_mfma_peak_probe", "svdq_linear_forward_static",
     "svdq_debug_launch_plan",
     "svdq_kv_cache_sizes", "svdq_kv_append", "svdq_kv_attention_workspace_bytes", "svdq_kv_attention", "svdq_kv_gather",
-    "svdq_kv_append_normed", "svdq_kv_attention_normed",
+    "svdq_kv_append_normed", "svdq_kv_attention_normed", "svdq_kv_compact_workspace_bytes", "svdq_kv_compact",
 ]
 
 
@@ -74,6 +74,10 @@ class KVRopeDev(C.Structure):
 
 class KVNormDev(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q_weight", "k_weight", "q_first", "k_first")] + [("first_tokens", C.c_int), ("per_head", C.c_int), ("eps", C.c_float)]
+
+
+class KVMovesDev(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("cu_moves", "from_token", "to_first", "from_table", "to_table")] + [(n, C.c_int) for n in ("sequences", "from_width", "to_width", "moves", "per_head")]
 
 
 class KVRowsDev(C.Structure):
@@ -143,6 +147,9 @@ def lib() -> C.CDLL:
         L.svdq_kv_append_normed.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), C.POINTER(KVNormDev), C.POINTER(KVRopeDev), C.POINTER(KVRowsDev), C.POINTER(KVRowsDev), vp]
         L.svdq_kv_attention_normed.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), C.POINTER(KVNormDev), C.POINTER(KVRopeDev), C.POINTER(KVRowsDev), C.c_int, C.c_float,
                                                C.c_int, C.c_int, C.c_int, vp, vp, C.c_size_t, vp]
+        L.svdq_kv_compact_workspace_bytes.restype = C.c_size_t
+        L.svdq_kv_compact_workspace_bytes.argtypes = [C.POINTER(KVShape), C.c_int, C.c_int]
+        L.svdq_kv_compact.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVCacheDev), C.POINTER(KVMovesDev), C.POINTER(KVRopeDev), vp, C.c_size_t, vp]
         L.svdq_kv_gather.argtypes = [C.POINTER(KVCacheDev), vp, vp, vp, C.c_int, C.c_int, C.c_int, vp, vp, vp]
         _lib = L
     return _lib

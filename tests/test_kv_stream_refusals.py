@@ -54,3 +54,41 @@ def test_first_tokens_below_zero_are_refused(lib):
 def test_the_plain_entry_points_refuse_as_before(lib):
     assert lib.svdq_kv_append(CACHE, BATCH, None, S.KVRowsDev(AT + 2, 256, 128), ROWS, None) == EINVAL
     assert lib.svdq_kv_attention(CACHE, BATCH, None, ROWS, 3, 0.1, 1, 0, AT, AT, C.c_size_t(1 << 40), None) == EINVAL
+
+
+# ---- compaction ------------------------------------------------------------------------------------------------------------------------------
+
+MOVES = dict(cu_moves=AT, from_token=AT, to_first=AT, from_table=AT, to_table=AT, sequences=3, from_width=5, to_width=4, moves=70, per_head=0)
+
+
+def moves(**other):
+    return S.KVMovesDev(**{**MOVES, **other})
+
+
+def cache(pages=4, heads=2, dim=128, page=64, k=AT):
+    return S.KVCacheDev(k, AT, AT, AT, pages, S.KVShape(heads, dim, page))
+
+
+@pytest.mark.parametrize("other,want", [
+    (dict(cu_moves=None), EINVAL), (dict(from_token=None), EINVAL), (dict(to_first=None), EINVAL), (dict(from_table=None), EINVAL), (dict(to_table=None), EINVAL),
+    (dict(from_token=AT + 2), EINVAL), (dict(to_table=AT + 1), EINVAL), (dict(from_table=AT + 3), EINVAL), (dict(from_width=0), EINVAL), (dict(to_width=0), EINVAL),
+    (dict(sequences=-1), EINVAL), (dict(moves=-1), EINVAL), (dict(from_width=-1), EINVAL), (dict(sequences=65536), EUNSUPPORTED),
+    (dict(from_width=(1 << 24) + 1), EUNSUPPORTED), (dict(to_width=(1 << 24) + 1), EUNSUPPORTED),
+])
+def test_moves_that_are_refused(lib, other, want):
+    assert lib.svdq_kv_compact(CACHE, CACHE, moves(**other), None, None, 0, None) == want
+
+
+def test_caches_and_workspaces_that_do_not_fit_are_refused(lib):
+    call = lambda to=CACHE, source=CACHE, m=MOVES, rope=None, at=None, size=0: lib.svdq_kv_compact(to, source, moves(**m), rope, at, C.c_size_t(size), None)
+    for other in (cache(heads=4), cache(dim=64), cache(pages=0), cache(k=AT + 8), cache(dim=96), cache(page=48)):
+        assert call(source=other) < 0 and call(to=other) < 0
+    need = lib.svdq_kv_compact_workspace_bytes(CACHE.shape, 3, 70)
+    assert need >= (70 // 32 + 6) * 2 * (64 * 128 + 2)
+    assert call(at=AT, size=need - 1) == ENOSPACE and call(at=AT + 128, size=need) == EINVAL
+    assert call(rope=S.KVRopeDev(AT, 5, 144, 0)) == EINVAL
+    for nothing in (dict(moves=0), dict(sequences=0)):
+        assert call(m=nothing) == 0 and call(source=cache(page=1024), m=nothing) == 0
+    assert lib.svdq_kv_compact(None, CACHE, moves(), None, None, 0, None) == EINVAL and lib.svdq_kv_compact(CACHE, CACHE, None, None, None, 0, None) == EINVAL
+    assert lib.svdq_kv_compact_workspace_bytes(S.KVShape(2, 96, 64), 3, 70) == 0 and lib.svdq_kv_compact_workspace_bytes(CACHE.shape, -1, 70) == 0
+    assert lib.svdq_kv_compact_workspace_bytes(CACHE.shape, 0, 0) > 0
