@@ -477,6 +477,42 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
                              size_t workspace_bytes, void *hip_stream);
 
 /*
+ * Pages that sequences share.  refs (svdq_kv_pool_dev; device, the caller's, zeros to begin with) counts for every page the table entries that name it; a page with none is free.  The
+ * functions below keep counts and tables in step, on the GPU alone: what they are called with is the program's whole use of those pages, and calls that share a pool or a table
+ * are ordered on one stream.  An entry outside 0 .. pages - 1 names no page.  One pool and one set of tables serve the caches of all layers.
+ *
+ * Release: entries of pages that lie wholly within tokens first_token[b] .. end_token[b] - 1 (NULL: from 0, to the end of the table) are given back: the counts go down, the
+ * entries become -1.  With (0, all) a sequence ends, with (its length, all) it is cut back, with (first tokens that stay visible, begin of the window) what a window left goes.
+ *
+ * Fork: row i of to_table becomes the pages that hold the tokens of row parent[i] of from_table, -1 behind them, and to_len[i] their number from_len[parent[i]] (up to what either
+ * table holds; nothing for a parent outside 0 .. from_sequences - 1); counts go up.  Several rows may have one parent.  What the rows of to_table named before is not given
+ * back: release it first.  The two tables, and the two arrays of lengths, do not overlap (SVDQ_EINVAL).
+ *
+ * Reserve: makes every page that the batch's new tokens fall in exist and be the sequence's own; call it before svdq_kv_append.  Among the entries of positions kv_len - n ..
+ * kv_len - 1, those that name no page, or one whose count is above one, get the lowest pages that were free at the call, in the order of sequences and entries; the old page's
+ * count goes down.  Of a page that held tokens before the new ones, those are copied, in whole blocks of 32, in `cache` if it is given; copies (NULL, or device int32 [sequences][3])
+ * says for each sequence (page, to page, tokens), (-1, -1, 0) if nothing is to be copied: with svdq_kv_copy_pages the caches of further layers follow.  missing (NULL, or device int32)
+ * becomes the number of entries for which no page was left: they name none (the tokens there are neither written nor seen, and those that a shared page held are lost to the
+ * sequence), nobody else's pages are touched.  workspace: device, 256-byte aligned, >= svdq_kv_pages_reserve_workspace_bytes(), no initial contents.  Two kernels; with the tables
+ * and counts of a captured graph's buffers it can be captured with the step.
+ *
+ * Copy: tokens c[i][2] (in whole blocks) of page c[i][0] of `from` to page c[i][1] of `to`; nothing where either names no page.  The caches are the same one or alike; no page is
+ * written twice, or written and read.
+ */
+typedef struct {
+    int32_t *refs; /* device [pages] */
+    int pages, page_tokens;
+} svdq_kv_pool_dev;
+int svdq_kv_pages_release(const svdq_kv_pool_dev *pool, int32_t *block_table, const int32_t *first_token, const int32_t *end_token,
+                          int sequences, int table_width, void *hip_stream);
+int svdq_kv_pages_fork(const svdq_kv_pool_dev *pool, const int32_t *from_table, const int32_t *from_len, int from_sequences, int from_width,
+                       const int32_t *parent, int32_t *to_table, int32_t *to_len, int sequences, int to_width, void *hip_stream);
+size_t svdq_kv_pages_reserve_workspace_bytes(const svdq_kv_pool_dev *pool, int sequences, int table_width);
+int svdq_kv_pages_reserve(const svdq_kv_pool_dev *pool, const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, int32_t *copies,
+                          int32_t *missing, void *workspace, size_t workspace_bytes, void *hip_stream);
+int svdq_kv_copy_pages(const svdq_kv_cache_dev *to, const svdq_kv_cache_dev *from, const int32_t *copies, int count, void *hip_stream);
+
+/*
  * Compaction: some of a sequence's tokens become its tokens from to_first[b] on, in the order in which they are given: token to_first[b] + i is what token
  * from_token[cu_moves[b] + i] was (with per_head: from_token[head][moves], a list for each head).  Any choice and order will do, a token may be taken twice.  Pages are those of
  * from_table for what is read, in the cache `from`, and of to_table for what is written, in `to` (the same cache or another one, of as many heads and the same head_dim).

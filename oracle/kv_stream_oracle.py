@@ -113,3 +113,56 @@ def moved_key(k, old, new, table, interleaved):
         both = 2.0 ** -20 * g * (np.abs(k[..., i]) + np.abs(k[..., j]))
         slack[..., i], slack[..., j] = both, both
     return out, np.where(stays, 0.0, slack)
+
+
+class Pages:
+    """Counts of pages and tables whose rows share them, one entry after another."""
+
+    def __init__(self, pages, page_tokens):
+        self.refs, self.P = [0] * pages, page_tokens
+
+    def page(self, g):
+        return 0 <= g < len(self.refs)
+
+    def release(self, table, first=None, end=None):
+        for b, row in enumerate(table):
+            for e, g in enumerate(row):
+                if e * self.P >= (0 if first is None else first[b]) and (end is None or (e + 1) * self.P <= end[b]):
+                    if self.page(g):
+                        self.refs[g] -= 1
+                    row[e] = -1
+
+    def fork(self, from_table, from_len, parent, to_table, to_len):
+        for i, p in enumerate(parent):
+            row, to_len[i] = to_table[i], 0
+            if 0 <= p < len(from_table):
+                to_len[i] = min(max(from_len[p], 0), min(len(from_table[p]), len(row)) * self.P)
+            for e in range(len(row)):
+                g = from_table[p][e] if e * self.P < to_len[i] else -1
+                row[e] = g if self.page(g) else -1
+                if self.page(g):
+                    self.refs[g] += 1
+
+    def reserve(self, table, new, lens):
+        """The copies (page, to page, tokens) of every sequence, and how many entries got no page."""
+        free = [g for g, n in enumerate(self.refs) if n <= 0]
+        was, missing, copies = list(self.refs), 0, []
+        for row, n, length in zip(table, new, lens):
+            length = min(max(length, 0), len(row) * self.P)
+            before = max(length - n, 0)
+            copy = (-1, -1, 0)
+            for e in range(before // self.P, (length + self.P - 1) // self.P) if n > 0 else ():
+                g = row[e]
+                if self.page(g) and was[g] <= 1:
+                    continue
+                if self.page(g):
+                    self.refs[g] -= 1
+                row[e] = free.pop(0) if free else -1
+                if row[e] < 0:
+                    missing += 1
+                    continue
+                self.refs[row[e]] = 1
+                if self.page(g) and e * self.P < before:
+                    copy = (g, row[e], before - e * self.P)
+            copies.append(copy)
+        return copies, missing

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsvdq.so")
 
 SOURCES = ["prepare.cpp", "act_kernel.hip", "act_onepass_kernel.hip", "act_w8_small_kernel.hip", "act_wide_kernel.hip", "act_tile_kernel.hip", "fused_small_kernel.hip", "gemm_w4a4_kernel.hip", "gemm_w4a4_kpar_kernel.hip", "gemm_w4a4_mid_kernel.hip", "gemm_fp4_kernel.hip", "gemm_kpar_blocks_kernel.hip", "w8a8_kernels.hip", "w4a16_kernel.hip", "peak_probe.hip", "api.hip",
-           "kv_cache_kernels.hip", "kv_rows_kernel.hip", "kv_tile_kernel.hip", "kv_compact_kernel.hip", "kv_api.hip"]
+           "kv_cache_kernels.hip", "kv_rows_kernel.hip", "kv_tile_kernel.hip", "kv_compact_kernel.hip", "kv_pages_kernel.hip", "kv_api.hip"]
 
 # -packed-fp32-ops is switched OFF for all device code; no fast-math, no fp contraction:
 # the quantizer's roundings must be exactly the IEEE single operations that are written.

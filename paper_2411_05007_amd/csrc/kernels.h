@@ -247,6 +247,32 @@ struct KvCompactParams {
     uint8_t *stage_bytes;    // [item][head][2]
 };
 hipError_t launch_kv_compact(const KvCompactParams &p, hipStream_t stream);
+struct KvPool {
+    int32_t *refs;           // [pages]: table entries that name the page
+    int pages, page_shift;
+};
+struct KvForkParams {
+    KvPool pool;
+    const int32_t *from_table, *from_len, *parent;      // [from_sequences][from_width], [from_sequences], [sequences]
+    int32_t *to_table, *to_len;      // [sequences][to_width], [sequences]
+    int from_sequences, from_width, sequences, to_width;
+};
+struct KvReservePlan { int slices, words; size_t slice_off, count_off, shared_off, lacks_off, total; };      // the workspace
+KvReservePlan plan_kv_reserve(int pages, int sequences, int width);
+struct KvReserveParams {
+    KvPool pool;
+    KvCache cache;           // k null: nothing is copied
+    KvBatch batch;           // its table is written
+    int32_t *copies;         // [sequences][3] or null: page, to page, tokens
+    int32_t *missing;        // or null
+    unsigned long long *free_words, *lacks;      // a bit a page; [sequences][words], a bit an entry
+    int32_t *slice_free, *lack_count, *shared;   // free pages of 1024; of a sequence the entries that lack a page, the page that it shares
+    int slices, words;
+};
+hipError_t launch_kv_release(const KvPool &pool, int32_t *table, const int32_t *first, const int32_t *last, int sequences, int width, hipStream_t stream);
+hipError_t launch_kv_fork(const KvForkParams &p, hipStream_t stream);
+hipError_t launch_kv_reserve(const KvReserveParams &p, hipStream_t stream);
+hipError_t launch_kv_copy_pages(const KvCache &to, const KvCache &from, const int32_t *copies, int n, hipStream_t stream);
 struct KvGatherParams {
     KvCache cache;
     KvBatch batch;

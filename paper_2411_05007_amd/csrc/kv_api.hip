@@ -67,6 +67,22 @@ svdq::KvNorm norm_of(const svdq_kv_norm *n, const float *weight, const float *fi
     return svdq::KvNorm{weight, first, n->per_head ? dim : 0, n->first_tokens, n->eps, 1};
 }
 svdq::KvRows rows_of(const svdq_kv_rows *r) { return svdq::KvRows{static_cast<const uint16_t *>(r->data), r->token_stride, r->head_stride}; }
+int check_pool(const svdq_kv_pool_dev *p) {
+    if (!p || !p->refs || ((uintptr_t)p->refs & 3) || p->pages <= 0 || p->page_tokens <= 0) return SVDQ_EINVAL;
+    return p->page_tokens < 32 || p->page_tokens > 1024 || (p->page_tokens & (p->page_tokens - 1)) ? SVDQ_EUNSUPPORTED : SVDQ_OK;
+}
+svdq::KvPool pool_of(const svdq_kv_pool_dev *p) { return svdq::KvPool{p->refs, p->pages, __builtin_ctz((unsigned)p->page_tokens)}; }
+// a table of `sequences` rows that is written
+int check_table(const int32_t *table, int sequences, int width, int page_tokens) {
+    if (sequences < 0 || width < 0) return SVDQ_EINVAL;
+    if (sequences == 0) return SVDQ_OK;
+    if (!table || ((uintptr_t)table & 3) || width == 0) return SVDQ_EINVAL;
+    return sequences > kMaxGridY || (long long)width * page_tokens > kMaxTokens ? SVDQ_EUNSUPPORTED : SVDQ_OK;
+}
+bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + b_bytes && y < x + a_bytes;
+}
 int done(hipError_t e) { return e == hipSuccess ? SVDQ_OK : svdq::record_hip_error(e); }
 
 }  // namespace
@@ -172,6 +188,73 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
     p.partial = reinterpret_cast<float *>(ws + plan.few_off);
     p.arrived = reinterpret_cast<unsigned long long *>(ws + plan.words_off);
     return done(svdq::launch_kv_attention_rows(p, stream));
+}
+
+int svdq_kv_pages_release(const svdq_kv_pool_dev *pool, int32_t *block_table, const int32_t *first_token, const int32_t *end_token, int sequences, int table_width,
+                          void *hip_stream) {
+    int st = check_pool(pool);
+    if (st != SVDQ_OK || (st = check_table(block_table, sequences, table_width, pool->page_tokens)) != SVDQ_OK) return st;
+    if (((uintptr_t)first_token | (uintptr_t)end_token) & 3) return SVDQ_EINVAL;
+    if (sequences == 0) return SVDQ_OK;
+    return done(svdq::launch_kv_release(pool_of(pool), block_table, first_token, end_token, sequences, table_width, static_cast<hipStream_t>(hip_stream)));
+}
+
+int svdq_kv_pages_fork(const svdq_kv_pool_dev *pool, const int32_t *from_table, const int32_t *from_len, int from_sequences, int from_width, const int32_t *parent,
+                       int32_t *to_table, int32_t *to_len, int sequences, int to_width, void *hip_stream) {
+    int st = check_pool(pool);
+    if (st != SVDQ_OK || (st = check_table(from_table, from_sequences, from_width, pool->page_tokens)) != SVDQ_OK ||
+        (st = check_table(to_table, sequences, to_width, pool->page_tokens)) != SVDQ_OK)
+        return st;
+    if (sequences == 0) return SVDQ_OK;
+    if (!parent || !to_len || (from_sequences > 0 && !from_len) || (((uintptr_t)from_len | (uintptr_t)parent | (uintptr_t)to_len) & 3)) return SVDQ_EINVAL;
+    // (rows are read while others are written)
+    const size_t from_bytes = (size_t)from_sequences * from_width * 4, to_bytes = (size_t)sequences * to_width * 4;
+    if (overlap(from_table, from_bytes, to_table, to_bytes) || overlap(from_len, (size_t)from_sequences * 4, to_len, (size_t)sequences * 4)) return SVDQ_EINVAL;
+    const svdq::KvForkParams p{pool_of(pool), from_table, from_len, parent, to_table, to_len, from_sequences, from_width, sequences, to_width};
+    return done(svdq::launch_kv_fork(p, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t svdq_kv_pages_reserve_workspace_bytes(const svdq_kv_pool_dev *pool, int sequences, int table_width) {
+    if (!pool || pool->pages <= 0 || sequences < 0 || table_width < 0) return 0;
+    return svdq::plan_kv_reserve(pool->pages, sequences, table_width).total;
+}
+
+int svdq_kv_pages_reserve(const svdq_kv_pool_dev *pool, const svdq_kv_cache_dev *cache, const svdq_kv_batch *batch, int32_t *copies, int32_t *missing, void *workspace,
+                          size_t workspace_bytes, void *hip_stream) {
+    int st = check_pool(pool);
+    if (st != SVDQ_OK || (cache && (st = check_cache(cache)) != SVDQ_OK)) return st;
+    if (!batch || (cache && (cache->pages < pool->pages || cache->shape.page_tokens != pool->page_tokens))) return SVDQ_EINVAL;
+    if ((st = check_tables(batch->cu_new, batch->kv_len, batch->block_table, batch->sequences, batch->table_width, batch->new_tokens, pool->page_tokens)) != SVDQ_OK) return st;
+    if (((uintptr_t)copies | (uintptr_t)missing) & 3) return SVDQ_EINVAL;
+    if (batch->sequences > 0 && (!batch->cu_new || !batch->kv_len || !batch->block_table || batch->table_width == 0 || !workspace || ((uintptr_t)workspace & 255))) return SVDQ_EINVAL;
+    if (batch->sequences > kMaxGridY) return SVDQ_EUNSUPPORTED;
+    if (batch->sequences == 0 && !missing) return SVDQ_OK;
+    const svdq::KvReservePlan plan = svdq::plan_kv_reserve(pool->pages, batch->sequences, batch->table_width);
+    if (batch->sequences > 0 && workspace_bytes < plan.total) return SVDQ_ENOSPACE;
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    svdq::KvReserveParams p{};
+    p.pool = pool_of(pool);
+    if (cache) p.cache = cache_of(cache);
+    p.batch = batch_of(batch);
+    p.copies = copies;
+    p.missing = missing;
+    p.free_words = reinterpret_cast<unsigned long long *>(ws);
+    p.slice_free = reinterpret_cast<int32_t *>(ws + plan.slice_off);
+    p.lack_count = reinterpret_cast<int32_t *>(ws + plan.count_off);
+    p.shared = reinterpret_cast<int32_t *>(ws + plan.shared_off);
+    p.lacks = reinterpret_cast<unsigned long long *>(ws + plan.lacks_off);
+    p.slices = plan.slices;
+    p.words = plan.words;
+    return done(svdq::launch_kv_reserve(p, static_cast<hipStream_t>(hip_stream)));
+}
+
+int svdq_kv_copy_pages(const svdq_kv_cache_dev *to, const svdq_kv_cache_dev *from, const int32_t *copies, int count, void *hip_stream) {
+    int st = check_cache(to);
+    if (st != SVDQ_OK || (st = check_cache(from)) != SVDQ_OK) return st;
+    if (to->shape.kv_heads != from->shape.kv_heads || to->shape.head_dim != from->shape.head_dim || to->shape.page_tokens != from->shape.page_tokens) return SVDQ_EINVAL;
+    if (count < 0 || (count > 0 && (!copies || ((uintptr_t)copies & 3)))) return SVDQ_EINVAL;
+    if (count == 0) return SVDQ_OK;
+    return done(svdq::launch_kv_copy_pages(cache_of(to), cache_of(from), copies, count, static_cast<hipStream_t>(hip_stream)));
 }
 
 size_t svdq_kv_compact_workspace_bytes(const svdq_kv_shape *shape, int sequences, int moves) {

@@ -197,6 +197,12 @@ class KVCache:
                                                   workspace.data_ptr(), workspace.numel(), self._stream(stream)), "svdq_kv_attention")
         return out
 
+    def copy_pages(self, copies, source: Optional["KVCache"] = None, stream=None) -> None:
+        """copies int32 [n, 3] on the GPU: page of `source` (None: of this cache), page of this cache, tokens (whole blocks of 32 are copied; rows that name no page are skipped)."""
+        _device_int32(copies, "copies")
+        assert copies.dim() == 2 and copies.shape[1] == 3, "copies: [n, 3]"
+        S._check(S.lib().svdq_kv_copy_pages(self.cdesc, (source or self).cdesc, copies.data_ptr(), copies.shape[0], self._stream(stream)), "svdq_kv_copy_pages")
+
     def compact_workspace(self, moves: KVMoves, stream=None):
         n = S.lib().svdq_kv_compact_workspace_bytes(C.byref(self.shape), moves.sequences, moves.moves)
         if n == 0:
@@ -221,3 +227,92 @@ class KVCache:
         S._check(S.lib().svdq_kv_gather(self.cdesc, *rows.pointers, rows.sequences, rows.width, rows.rows, out[0].data_ptr(), out[1].data_ptr(), self._stream(stream)),
                  "svdq_kv_gather")
         return out
+
+
+class KVPages:
+    """Which pages are in use, by how many table entries, on the GPU: tables whose rows share pages are changed by fork(), reserve() and release() alone.
+
+        pool = KVPages(pages, page_tokens)                   # one for the caches of all layers
+        pool.fork(table, kv_len, parent, branch_table, branch_len)      # branches share the pages of their parents
+        pool.reserve(cache, batch)                           # before append(): the new tokens' pages exist and are the sequence's own
+        pool.release(branch_table)                           # given back
+    """
+
+    def __init__(self, pages: int, page_tokens: int = 64, device: str = "cuda:0"):
+        if not torch.cuda.is_available():
+            raise S.SvdqError("no GPU visible: the pages have no CPU path")
+        self._own(torch.zeros(pages, dtype=torch.int32, device=device), page_tokens)
+
+    @classmethod
+    def from_counts(cls, refs, page_tokens: int = 64) -> "KVPages":
+        """Over counts int32 [pages] that are there already; they are kept, not copied."""
+        self = cls.__new__(cls)
+        self._own(refs, page_tokens)
+        return self
+
+    def _own(self, refs, page_tokens: int) -> None:
+        _device_int32(refs, "refs")
+        assert refs.dim() == 1
+        self.refs, self.pages, self.page_tokens, self.device = refs, refs.shape[0], int(page_tokens), refs.device
+        self.cdesc = S.KVPoolDev(refs.data_ptr(), self.pages, self.page_tokens)
+
+    _stream, _new = KVCache._stream, KVCache._new
+
+    @staticmethod
+    def _table(t, name: str) -> None:
+        _device_int32(t, name)
+        assert t.dim() == 2, f"{name}: [sequences, width]"
+
+    def release(self, block_table, first_token=None, end_token=None, stream=None) -> None:
+        """Gives back the pages wholly within tokens first_token[b] .. end_token[b] - 1 of each row (None: from 0, to the end); the entries become -1."""
+        self._table(block_table, "block_table")
+        at = [None, None]
+        for i, t in enumerate((first_token, end_token)):
+            if t is not None:
+                _device_int32(t, ("first_token", "end_token")[i])
+                assert t.shape == (block_table.shape[0],)
+                at[i] = t.data_ptr()
+        S._check(S.lib().svdq_kv_pages_release(self.cdesc, block_table.data_ptr(), *at, *block_table.shape, self._stream(stream)), "svdq_kv_pages_release")
+
+    def fork(self, from_table, from_len, parent, to_table, to_len, stream=None) -> None:
+        """Rows of to_table take the pages of rows parent[i] of from_table, to_len[i] becomes from_len[parent[i]].  What to_table named before is to be released first."""
+        self._table(from_table, "from_table")
+        self._table(to_table, "to_table")
+        for t, n, rows in ((from_len, "from_len", from_table), (parent, "parent", to_table), (to_len, "to_len", to_table)):
+            _device_int32(t, n)
+            assert t.shape == (rows.shape[0],), f"{n}: one for each row"
+        S._check(S.lib().svdq_kv_pages_fork(self.cdesc, from_table.data_ptr(), from_len.data_ptr(), *from_table.shape, parent.data_ptr(), to_table.data_ptr(), to_len.data_ptr(),
+                                            *to_table.shape, self._stream(stream)), "svdq_kv_pages_fork")
+
+    def reserve_workspace(self, batch: KVBatch, stream=None):
+        """For reserve(): its notes, and what further caches copy."""
+        return self._new(self._notes(batch) + 12 * batch.sequences, torch.uint8, stream)
+
+    def _notes(self, batch: KVBatch) -> int:
+        n = S.lib().svdq_kv_pages_reserve_workspace_bytes(C.byref(self.cdesc), batch.sequences, batch.block_table.shape[1])
+        if n == 0:
+            raise S.SvdqError("unsupported pool")
+        return n
+
+    def reserve(self, cache, batch: KVBatch, missing=None, workspace=None, stream=None) -> None:
+        """Pages of its own for every new token of the batch, whose block_table is written; tokens before them in a shared page are copied, in `cache` or, where layers
+        have caches of their own, in each of a list of them.  missing: int32 [1] on the GPU, entries for which no page was left (they name none)."""
+        caches = [cache] if isinstance(cache, KVCache) else list(cache)
+        if missing is not None:
+            _device_int32(missing, "missing")
+            assert missing.numel() == 1
+        if workspace is None:
+            workspace = self.reserve_workspace(batch, stream)
+        else:
+            assert workspace.dtype is torch.uint8 and workspace.is_cuda and workspace.is_contiguous(), "workspace: uint8 on the GPU"
+        L, at, size, copies = S.lib(), workspace.data_ptr(), workspace.numel(), None
+        if len(caches) > 1:
+            size = self._notes(batch)
+            if workspace.numel() < size + 12 * batch.sequences:
+                raise S.SvdqError("svdq_kv_pages_reserve: workspace smaller than reserve_workspace()")
+            copies = at + size
+        s = self._stream(stream)
+        S._check(L.svdq_kv_pages_reserve(self.cdesc, caches[0].cdesc if caches else None, batch.cdesc, copies, None if missing is None else missing.data_ptr(), at, size, s),
+                 "svdq_kv_pages_reserve")
+        for c in caches[1:]:
+            S._check(L.svdq_kv_copy_pages(c.cdesc, c.cdesc, copies, batch.sequences, s), "svdq_kv_copy_pages")

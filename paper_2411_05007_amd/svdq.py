@@ -33,6 +33,7 @@ EXPORTS = [
     "svdq_debug_launch_plan",
     "svdq_kv_cache_sizes", "svdq_kv_append", "svdq_kv_attention_workspace_bytes", "svdq_kv_attention", "svdq_kv_gather",
     "svdq_kv_append_normed", "svdq_kv_attention_normed", "svdq_kv_compact_workspace_bytes", "svdq_kv_compact",
+    "svdq_kv_pages_release", "svdq_kv_pages_fork", "svdq_kv_pages_reserve_workspace_bytes", "svdq_kv_pages_reserve", "svdq_kv_copy_pages",
 ]
 
 
@@ -74,6 +75,10 @@ class KVRopeDev(C.Structure):
 
 class KVNormDev(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q_weight", "k_weight", "q_first", "k_first")] + [("first_tokens", C.c_int), ("per_head", C.c_int), ("eps", C.c_float)]
+
+
+class KVPoolDev(C.Structure):
+    _fields_ = [("refs", C.c_void_p), ("pages", C.c_int), ("page_tokens", C.c_int)]
 
 
 class KVMovesDev(C.Structure):
@@ -147,6 +152,12 @@ def lib() -> C.CDLL:
         L.svdq_kv_append_normed.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), C.POINTER(KVNormDev), C.POINTER(KVRopeDev), C.POINTER(KVRowsDev), C.POINTER(KVRowsDev), vp]
         L.svdq_kv_attention_normed.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), C.POINTER(KVNormDev), C.POINTER(KVRopeDev), C.POINTER(KVRowsDev), C.c_int, C.c_float,
                                                C.c_int, C.c_int, C.c_int, vp, vp, C.c_size_t, vp]
+        L.svdq_kv_pages_release.argtypes = [C.POINTER(KVPoolDev), vp, vp, vp, C.c_int, C.c_int, vp]
+        L.svdq_kv_pages_fork.argtypes = [C.POINTER(KVPoolDev), vp, vp, C.c_int, C.c_int, vp, vp, vp, C.c_int, C.c_int, vp]
+        L.svdq_kv_pages_reserve_workspace_bytes.restype = C.c_size_t
+        L.svdq_kv_pages_reserve_workspace_bytes.argtypes = [C.POINTER(KVPoolDev), C.c_int, C.c_int]
+        L.svdq_kv_pages_reserve.argtypes = [C.POINTER(KVPoolDev), C.POINTER(KVCacheDev), C.POINTER(KVBatchDev), vp, vp, vp, C.c_size_t, vp]
+        L.svdq_kv_copy_pages.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVCacheDev), vp, C.c_int, vp]
         L.svdq_kv_compact_workspace_bytes.restype = C.c_size_t
         L.svdq_kv_compact_workspace_bytes.argtypes = [C.POINTER(KVShape), C.c_int, C.c_int]
         L.svdq_kv_compact.argtypes = [C.POINTER(KVCacheDev), C.POINTER(KVCacheDev), C.POINTER(KVMovesDev), C.POINTER(KVRopeDev), vp, C.c_size_t, vp]

@@ -92,3 +92,52 @@ def test_caches_and_workspaces_that_do_not_fit_are_refused(lib):
     assert lib.svdq_kv_compact(None, CACHE, moves(), None, None, 0, None) == EINVAL and lib.svdq_kv_compact(CACHE, CACHE, None, None, None, 0, None) == EINVAL
     assert lib.svdq_kv_compact_workspace_bytes(S.KVShape(2, 96, 64), 3, 70) == 0 and lib.svdq_kv_compact_workspace_bytes(CACHE.shape, -1, 70) == 0
     assert lib.svdq_kv_compact_workspace_bytes(CACHE.shape, 0, 0) > 0
+
+
+# ---- pages -----------------------------------------------------------------------------------------------------------------------------------
+
+
+def pool(refs=AT, pages=4, page=64):
+    return S.KVPoolDev(refs, pages, page)
+
+
+FAR = AT + (1 << 20)
+
+
+@pytest.mark.parametrize("p,want", [(pool(refs=None), EINVAL), (pool(refs=AT + 2), EINVAL), (pool(pages=0), EINVAL), (pool(pages=-3), EINVAL), (pool(page=0), EINVAL),
+                                    (pool(page=16), EUNSUPPORTED), (pool(page=96), EUNSUPPORTED), (pool(page=2048), EUNSUPPORTED)])
+def test_pools_that_are_refused(lib, p, want):
+    assert lib.svdq_kv_pages_release(p, AT, None, None, 3, 5, None) == want
+    assert lib.svdq_kv_pages_fork(p, AT, AT, 3, 5, AT, FAR, FAR, 3, 5, None) == want
+    assert lib.svdq_kv_pages_reserve(p, None, BATCH, None, None, AT, C.c_size_t(1 << 40), None) == want
+
+
+def test_tables_that_are_refused(lib):
+    release = lambda table=AT, first=None, end=None, n=3, width=5: lib.svdq_kv_pages_release(pool(), table, first, end, n, width, None)
+    assert release(table=None) == release(table=AT + 2) == release(first=AT + 1) == release(end=AT + 3) == release(n=-1) == release(width=0) == release(width=-1) == EINVAL
+    assert release(n=65536) == release(width=(1 << 24) + 1) == EUNSUPPORTED
+    assert release(n=0) == 0 and release(table=None, n=0) == 0
+    fork = lambda f=AT, fl=AT, n=3, fw=5, parent=AT, t=FAR, tl=FAR, m=4, tw=6: lib.svdq_kv_pages_fork(pool(), f, fl, n, fw, parent, t, tl, m, tw, None)
+    assert fork(f=None) == fork(fl=None) == fork(parent=None) == fork(t=None) == fork(tl=None) == fork(f=AT + 1) == fork(fl=AT + 2) == fork(tl=FAR + 2) == fork(n=-1) == EINVAL
+    assert fork(t=AT) == fork(t=AT + 56) == fork(f=FAR + 92) == fork(tl=AT) == fork(tl=AT + 8) == EINVAL      # the tables, or the lengths, overlap
+    assert fork(m=65536) == fork(n=65536) == fork(tw=(1 << 24) + 1) == EUNSUPPORTED
+    assert fork(m=0) == 0
+
+
+def test_reservations_that_are_refused(lib):
+    p = pool()
+    need = lib.svdq_kv_pages_reserve_workspace_bytes(p, 3, 2)
+    call = lambda c=CACHE, b=BATCH, copies=None, missing=None, at=AT, size=1 << 40: lib.svdq_kv_pages_reserve(p, c, b, copies, missing, at, C.c_size_t(size), None)
+    batch = lambda **o: S.KVBatchDev(*{**dict(cu=AT, len=AT, table=AT, sequences=3, width=2, new=5, max_new=4, max_len=100), **o}.values())
+    assert call(copies=AT + 2) == call(missing=AT + 1) == call(at=None) == call(at=AT + 128) == EINVAL
+    assert call(c=cache(pages=3)) == call(c=cache(page=128)) == EINVAL
+    assert call(size=need - 1) == ENOSPACE
+    assert call(b=batch(cu=None)) == call(b=batch(len=None)) == call(b=batch(table=None)) == call(b=batch(sequences=-1)) == call(b=batch(new=-1)) == call(b=batch(width=0)) == EINVAL
+    assert call(b=batch(table=None, new=0)) == call(b=batch(cu=None, new=0)) == EINVAL      # (no tokens: missing is counted all the same)
+    assert call(b=batch(sequences=65536)) == EUNSUPPORTED
+    assert call(b=batch(sequences=0), at=None, size=0) == 0
+    assert lib.svdq_kv_pages_reserve_workspace_bytes(pool(pages=0), 3, 2) == 0 and lib.svdq_kv_pages_reserve_workspace_bytes(p, -1, 2) == 0
+    assert lib.svdq_kv_copy_pages(CACHE, CACHE, None, 3, None) == lib.svdq_kv_copy_pages(CACHE, CACHE, AT + 1, 3, None) == lib.svdq_kv_copy_pages(CACHE, CACHE, AT, -1, None) == EINVAL
+    for other in (cache(heads=4), cache(dim=64), cache(page=128)):
+        assert lib.svdq_kv_copy_pages(CACHE, other, AT, 3, None) == EINVAL
+    assert lib.svdq_kv_copy_pages(CACHE, CACHE, None, 0, None) == 0
