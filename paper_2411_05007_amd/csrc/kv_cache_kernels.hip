@@ -24,6 +24,8 @@
 namespace svdq {
 namespace {
 
+constexpr int kAppendHeads = 4;      // of a workgroup, at most
+
 // The keys of half a block, 16 tokens.  A unit is 16 channels of a token, the two runs of eight that the rotation pairs; a lane has N of them.
 // (Per head and wavefront the instructions are what counts: places are found once for all heads, relative to a base that is the same for all lanes.)
 template <int D, bool NORM>
@@ -36,10 +38,25 @@ struct KeySide {
     uint32_t from[N][2], to[N][2];      // places in the rows, from there, and in the codes of a block
     uint32_t raw[kRaw];
     float c[N][8], s[N][8], x[N][2][8];
-    float weight[NORM ? N : 1][2][8];      // of the norm
+    const float *weights;         // of the norm, in LDS: [of all tokens, of the first][head][D]
+    int chan[2], heads, h0;       // the unit's two runs; heads that weights lie there of
     float top[N];
     __device__ __forceinline__ int token(int i) const { return 16 * half + (lane + 64 * i) / U; }
-    __device__ __forceinline__ KeySide(const KvAppendParams &p_, const BlockWork &w_, int lane_, int half_) : p(p_), w(w_), lane(lane_), half(half_) {
+    __device__ __forceinline__ KeySide(const KvAppendParams &p_, const BlockWork &w_, int lane_, int half_, float *lds, int h0_, int h1) : p(p_), w(w_), lane(lane_), half(half_), h0(h0_) {
+        if (NORM) {      // (each wavefront has a copy of its own: nothing to wait for)
+            heads = p.norm.head_stride ? h1 - h0 : 1;
+            float *mine = lds + half * (2 * kAppendHeads * D);
+            weights = mine;
+            for (int i = lane * 4; i < 2 * heads * D; i += 256) {
+                const float *row = i < heads * D ? p.norm.weight : p.norm.first;
+                const int at = i < heads * D ? i : i - heads * D;
+                *reinterpret_cast<kv_floatx4 *>(mine + i) = row ? *reinterpret_cast<const kv_floatx4 *>(row + (size_t)h0 * p.norm.head_stride + at) : kv_floatx4{1.f, 1.f, 1.f, 1.f};
+            }
+            const int pr = lane % U;
+            const bool halves = !p.rope.interleaved && pr < p.rope.dims / 16;
+            chan[0] = halves ? pr * 8 : pr * 16;
+            chan[1] = halves ? pr * 8 + p.rope.dims / 2 : pr * 16 + 8;
+        }
         base = p.k.data + (w.row0 + w.lo) * p.k.token_stride;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -53,22 +70,7 @@ struct KeySide {
             }
         }
     }
-    __device__ __forceinline__ void load_weights(int h) {
-#pragma unroll
-        for (int i = 0; i < (NORM ? N : 0); ++i) {
-            const int pr = (lane + 64 * i) % U, pos = w.blk * kKvBlock + readable(w, token(i));
-            const bool halves = !p.rope.interleaved && pr < p.rope.dims / 16;
-            const float *row = kv_norm_row(p.norm, pos, h);
-            kv_load_weights(row, halves ? pr * 8 : pr * 16, weight[NORM ? i : 0][0]);
-            kv_load_weights(row, halves ? pr * 8 + p.rope.dims / 2 : pr * 16 + 8, weight[NORM ? i : 0][1]);
-        }
-    }
-    // what is each head's own, once the last one's is used
-    __device__ __forceinline__ void load_next(int h) {
-        if (NORM && p.norm.head_stride != 0) load_weights(h);
-    }
-    __device__ __forceinline__ void load_common(int h0) {      // the same for all heads
-        load_weights(h0);
+    __device__ __forceinline__ void load_common() {      // the same for all heads
         if (p.rope.dims == 0) return;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -89,28 +91,37 @@ struct KeySide {
             }
     }
     __device__ __forceinline__ void load_old(long long) {}
+    static __device__ __forceinline__ float turn_a(float a, float b, float c, float s) { return NORM ? kv_turn_fma_a(a, b, c, s) : kv_turn_a(a, b, c, s); }
+    static __device__ __forceinline__ float turn_b(float a, float b, float c, float s) { return NORM ? kv_turn_fma_b(a, b, c, s) : kv_turn_b(a, b, c, s); }
     // turns the rows; returns the tokens with an element that is not finite (top: largest magnitude of a unit)
-    __device__ __forceinline__ uint32_t look() {
+    __device__ __forceinline__ uint32_t look(int h) {
         uint32_t bad = 0u;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             kv_floats(make_uint4(raw[i * 8], raw[i * 8 + 1], raw[i * 8 + 2], raw[i * 8 + 3]), x[i][0]);
             kv_floats(make_uint4(raw[i * 8 + 4], raw[i * 8 + 5], raw[i * 8 + 6], raw[i * 8 + 7]), x[i][1]);
-            if (NORM) kv_normalise<U>(x[i], weight[NORM ? i : 0], p.norm.eps);
+            if (NORM) {
+                const int pos = w.blk * kKvBlock + readable(w, token(i));
+                const float *row = weights + ((pos < p.norm.first_tokens ? heads : 0) + (p.norm.head_stride ? h - h0 : 0)) * D;
+                float weight[2][8];
+                kv_load8(row + chan[0], weight[0]);
+                kv_load8(row + chan[1], weight[1]);
+                kv_normalise<U>(x[i], weight, p.norm.eps);
+            }
             if ((lane + 64 * i) % U < p.rope.dims / 16) {
                 if (p.rope.interleaved) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float a = x[i][e / 4][2 * (e % 4)], y = x[i][e / 4][2 * (e % 4) + 1];
-                        x[i][e / 4][2 * (e % 4)] = kv_turn_a(a, y, c[i][e], s[i][e]);
-                        x[i][e / 4][2 * (e % 4) + 1] = kv_turn_b(a, y, c[i][e], s[i][e]);
+                        x[i][e / 4][2 * (e % 4)] = turn_a(a, y, c[i][e], s[i][e]);
+                        x[i][e / 4][2 * (e % 4) + 1] = turn_b(a, y, c[i][e], s[i][e]);
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float a = x[i][0][e], y = x[i][1][e];
-                        x[i][0][e] = kv_turn_a(a, y, c[i][e], s[i][e]);
-                        x[i][1][e] = kv_turn_b(a, y, c[i][e], s[i][e]);
+                        x[i][0][e] = turn_a(a, y, c[i][e], s[i][e]);
+                        x[i][1][e] = turn_b(a, y, c[i][e], s[i][e]);
                     }
                 }
             }
@@ -170,7 +181,7 @@ struct ValueSide {
     uint32_t raw[kRaw];
     uint2 old[E];
     __device__ __forceinline__ int token(int j) const { return kv_slot_token(slot) + (j & 3) + 8 * (j >> 2); }
-    __device__ __forceinline__ ValueSide(const KvAppendParams &p_, const BlockWork &w_, int lane_, int half_) : p(p_), w(w_), lane(lane_), half(half_), slot(2 * half_ + (lane_ & 1)) {
+    __device__ __forceinline__ ValueSide(const KvAppendParams &p_, const BlockWork &w_, int lane_, int half_, float *, int, int) : p(p_), w(w_), lane(lane_), half(half_), slot(2 * half_ + (lane_ & 1)) {
         const int a = (lane >> 2) / Q, c = (lane >> 1) & 1, q = (lane >> 2) % Q;
         base = p.v.data + (w.row0 + w.lo) * p.v.token_stride;
         to = (uint32_t)(((a * 16 + E * q) * 4 + slot) * 16 + 8 * c);
@@ -182,8 +193,7 @@ struct ValueSide {
             if (token(j) < w.lo) keep[j >> 2] |= 0xffu << (8 * (j & 3));
         }
     }
-    __device__ __forceinline__ void load_common(int) {}
-    __device__ __forceinline__ void load_next(int) {}
+    __device__ __forceinline__ void load_common() {}
     __device__ __forceinline__ void load(uint32_t (&r)[kRaw], int h) const {
         const uint16_t *head = base + h * p.v.head_stride;
 #pragma unroll
@@ -204,7 +214,7 @@ struct ValueSide {
         for (int i = 1; i < W; ++i) m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2_t, m), __builtin_bit_cast(ushort2_t, raw[j * W + i] & 0x7fff7fffu)));
         return live(w, token(j)) ? m : 0u;
     }
-    __device__ __forceinline__ uint32_t look() {
+    __device__ __forceinline__ uint32_t look(int) {
         uint32_t m = 0u;
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2_t, m), __builtin_bit_cast(ushort2_t, largest_of(j))));
@@ -254,10 +264,10 @@ struct ValueSide {
 // Rows first, then what waits for the block table; the rows of the next head are requested before this one's are worked on.  The four wavefronts' masks and
 // maxima meet once a head.
 template <typename Side>
-__device__ __forceinline__ void append_heads(const KvAppendParams &p, const BlockWork &w, int sequence, int h0, int h1, uint8_t *scales, int wave, Exchange (&exchange)[2]) {
-    Side side(p, w, (int)threadIdx.x & 63, wave & 1);
+__device__ __forceinline__ void append_heads(const KvAppendParams &p, const BlockWork &w, int sequence, int h0, int h1, uint8_t *scales, int wave, Exchange (&exchange)[2], float *lds) {
+    Side side(p, w, (int)threadIdx.x & 63, wave & 1, lds, h0, h1);
     side.load(side.raw, h0);
-    side.load_common(h0);
+    side.load_common();
     const long long unit0 = kv_unit(p.cache, p.batch.table, p.batch.table_width, sequence, h0, w.blk);
     if (unit0 < 0) return;     // (all wavefronts)
     for (int h = h0; h < h1; ++h) {
@@ -268,8 +278,7 @@ __device__ __forceinline__ void append_heads(const KvAppendParams &p, const Bloc
         const int held = tells && w.lo > 0 ? (int)scales[unit] : 0;
         side.load_old(unit);
         Exchange &ex = exchange[h & 1];      // (written again two heads on: behind a barrier that every wavefront enters when it has read it)
-        const uint32_t bad = side.look(), most = side.largest(bad);
-        side.load_next(h + 1 < h1 ? h + 1 : h);
+        const uint32_t bad = side.look(h), most = side.largest(bad);
         if (side.lane == 0) {
             ex.bad[wave] = bad;
             ex.top[wave] = most;
@@ -292,8 +301,9 @@ __device__ __forceinline__ void append_heads(const KvAppendParams &p, const Bloc
 }
 
 template <int D, bool NORM>
-__global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p, int heads_per_wg) {
+__global__ __launch_bounds__(256, NORM && D == 128 ? 4 : 1) void kv_append_kernel(KvAppendParams p, int heads_per_wg) {
     __shared__ Exchange exchange[2];
+    __shared__ __attribute__((aligned(16))) float weights[NORM ? 2 * 2 * kAppendHeads * D : 1];
     const KvItem item = kv_item(p.batch, blockIdx.x, [&](int n, int value) {
         const int len = kv_length(p.cache, p.batch, value), first = len > n ? len - n : 0;
         return n > 0 ? ((len + 31) >> 5) - (first >> 5) : 0;
@@ -308,8 +318,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p, int he
     w.row0 = (long long)item.first + (w.blk * kKvBlock - before);      // input row of the block's token 0 (rows lo .. hi - 1 are read)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h0 = blockIdx.y * heads_per_wg, h1 = h0 + heads_per_wg < p.cache.heads ? h0 + heads_per_wg : p.cache.heads;
-    if (wave < 2) append_heads<KeySide<D, NORM>>(p, w, item.sequence, h0, h1, p.cache.ks, wave, exchange);
-    else append_heads<ValueSide<D>>(p, w, item.sequence, h0, h1, p.cache.vs, wave, exchange);
+    if (wave < 2) append_heads<KeySide<D, NORM>>(p, w, item.sequence, h0, h1, p.cache.ks, wave, exchange, weights);
+    else append_heads<ValueSide<D>>(p, w, item.sequence, h0, h1, p.cache.vs, wave, exchange, weights);
 }
 
 // Gather: rows of the cache as bf16, code * 2^(byte - 127), exact where the product is a normal bf16.  Wavefront 0 has a block's keys, wavefront 1 its values:
@@ -394,7 +404,7 @@ hipError_t launch_kv_append(const KvAppendParams &p, hipStream_t stream) {
     // Heads a workgroup: one while there are fewer workgroups than stay on the chip together (256 CUs, four each), then more, up to four, which saves what is the
     // same for all heads.  1, 2, 4 heads: 64 items of 8 heads of 128 7.4, 7.5, 9.5 us; 190 of 12 of 64 11.2, 10.1, 11.5 us; 580 of 24 of 128 103, 88, 83 us.
     const long long rounds = (long long)items * p.cache.heads / 1024;
-    const int most = rounds < 1 ? 1 : rounds > 4 ? 4 : (int)rounds, per = most < p.cache.heads ? most : p.cache.heads;
+    const int most = rounds < 1 ? 1 : rounds > kAppendHeads ? kAppendHeads : (int)rounds, per = most < p.cache.heads ? most : p.cache.heads;
     const dim3 grid(items, (p.cache.heads + per - 1) / per);
     const auto kernel = p.cache.dim == 64    ? p.norm.on ? kv_append_kernel<64, true> : kv_append_kernel<64, false>
                         : p.cache.dim == 128 ? p.norm.on ? kv_append_kernel<128, true> : kv_append_kernel<128, false>

@@ -133,11 +133,18 @@ __device__ __forceinline__ void kv_load8(const float *p, float (&x)[8]) {
 // Two channels of a pair: (a, b) -> (a c - b s, b c + a s), each product and the sum rounded once (the build contracts nothing).
 __device__ __forceinline__ float kv_turn_a(float a, float b, float c, float s) { return a * c - b * s; }
 __device__ __forceinline__ float kv_turn_b(float a, float b, float c, float s) { return b * c + a * s; }
+// The same with one product left unrounded, for what other roundings come before.
+__device__ __forceinline__ float kv_turn_fma_a(float a, float b, float c, float s) { return __builtin_fmaf(a, c, -(b * s)); }
+__device__ __forceinline__ float kv_turn_fma_b(float a, float b, float c, float s) { return __builtin_fmaf(b, c, a * s); }
 
 // ---- norm of a head: y = x r w with r = 1 / sqrt(mean x^2 + eps), before the rotation ---------------------------------------------
 // Squares of numbers past 2^60 may leave fp32: rows whose sum does are taken 2^-72 times (eps is nothing beside them) and summed again, which happens in no ordinary call.
 constexpr float kKvTiny = 2.1175823681357508e-22f;      // 2^-72
-__device__ __forceinline__ float kv_norm_factor(float sum, float inv_dim, float eps) { return __builtin_amdgcn_rsqf(sum * inv_dim + eps); }      // within an ulp
+__device__ __forceinline__ float kv_norm_factor(float sum, float inv_dim, float eps) {      // within half an ulp and little: a step of Newton's on the instruction's
+    const float m = sum * inv_dim + eps, r = __builtin_amdgcn_rsqf(m);
+    const float e = __builtin_fmaf(-(m * r), r, 1.f);
+    return __builtin_fmaf(0.5f * r, e, r);
+}
 // weights of a token and head, null: ones
 __device__ __forceinline__ const float *kv_norm_row(const KvNorm &n, int pos, int head) {
     const float *w = pos < n.first_tokens ? n.first : n.weight;
@@ -151,10 +158,14 @@ __device__ __forceinline__ void kv_load_weights(const float *row, int at, float 
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = 1.f;
 }
-__device__ __forceinline__ float kv_squares(float sum, const float (&x)[8]) {
+__device__ __forceinline__ float kv_squares(const float (&x)[8]) {      // two sums of four: a chain half as long
+    float a = x[0] * x[0], b = x[4] * x[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
-    return sum;
+    for (int e = 1; e < 4; ++e) {
+        a = __builtin_fmaf(x[e], x[e], a);
+        b = __builtin_fmaf(x[4 + e], x[4 + e], b);
+    }
+    return a + b;
 }
 
 // Eight channels at each of N places of one row of 16-bit queries at position `pos`, rotated, in fp32; place(i) is a multiple of 8.  In the order of halves
@@ -286,14 +297,14 @@ __device__ __forceinline__ float kv_sum_lanes(float x) {
 template <int U>
 __device__ __forceinline__ void kv_normalise(float (&x)[2][8], const float (&w)[2][8], float eps) {
     constexpr float kInverse = 1.f / (16 * U);
-    float sum = kv_sum_lanes<U>(kv_squares(kv_squares(0.f, x[0]), x[1]));
+    float sum = kv_sum_lanes<U>(kv_squares(x[0]) + kv_squares(x[1]));
     const bool large = !(sum < __builtin_inff());
     if (__builtin_amdgcn_ballot_w64(large) != 0ull) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[j][e] = large ? x[j][e] * kKvTiny : x[j][e];
-        sum = kv_sum_lanes<U>(kv_squares(kv_squares(0.f, x[0]), x[1]));
+        sum = kv_sum_lanes<U>(kv_squares(x[0]) + kv_squares(x[1]));
         eps = large ? 0.f : eps;
     }
     const float r = kv_norm_factor(sum, kInverse, eps);

@@ -67,6 +67,9 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     const auto hi_of = [&](int at) { return at < 0 ? 0 : p.causal ? at + 1 : len; };      // (a token without a position sees nothing)
     const int seen_hi = hi_of(pos);
     const int seen_lo = p.causal && p.window > 0 && pos + 1 > p.window ? pos + 1 - p.window : 0;
+    // keys of the row between the first tokens and its window
+    const int hidden = MORE && p.sinks < seen_lo ? p.sinks : seen_lo;
+    const uint32_t hidden_count = (uint32_t)(seen_lo - hidden);
     // of the tile: its first row sees the fewest and the earliest keys
     const int tok_a = tile * 16 / p.group, last = tile * 16 + 15 < rows ? tile * 16 + 15 : rows - 1, tok_z = last / p.group;
     const int pos_a = len - n + tok_a, pos_z = len - n + tok_z;
@@ -148,9 +151,11 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
                 for (int c = 0; c < C; ++c) {
                     float y[8];
                     kv_floats(whole[MORE ? c : 0], y);
+                    if (by != 1.f) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] *= by;
-                    sum = kv_squares(sum, y);
+                        for (int e = 0; e < 8; ++e) y[e] *= by;
+                    }
+                    sum += kv_squares(y);
                 }
                 return kv_sum32(kv_sum16(sum));
             };
@@ -209,7 +214,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
 
     // exponents t of block i's weights, -inf where the row does not see the token; values of tokens that do not exist are cleared
     auto scores = [&](Block<D> &cur, int i, float (&t)[8]) {
-        const int blk = block_of(base + WAVES * i), kb = __builtin_amdgcn_readlane(kb_l, i);
+        const int v = base + WAVES * i, blk = block_of(v), kb = __builtin_amdgcn_readlane(kb_l, i);
         const bool named = __builtin_amdgcn_readlane(page_l, i) >= 0;
         kv_floatx4 s[2] = {};
 #pragma unroll
@@ -223,13 +228,13 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
         const float f = kv_within_range(to_t * kv_pow2(kb - 127));      // (a sum of zero times it is zero)
 #pragma unroll
         for (int j = 0; j < 8; ++j) t[j] = s[j / 4][j % 4] * f;
-        if (!named || blk * kKvBlock < all_lo || blk * kKvBlock + kKvBlock > all_hi) {
+        if (!named || v * kKvBlock < all_lo || v * kKvBlock + kKvBlock > all_hi) {      // (before the window: less than all_lo)
             const int first = blk * kKvBlock + kv_slot_token(q4);
             uint32_t live[2] = {~0u, ~0u};       // bytes of the codes of tokens that exist
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int key = first + (j & 3) + 8 * (j >> 2);
-                const bool ok = named && (key >= seen_lo || (MORE && key < sinks)) && key < seen_hi && key < len;
+                const bool ok = named && (MORE ? (uint32_t)(key - hidden) >= hidden_count : key >= seen_lo) && key < seen_hi && key < len;
                 t[j] = ok ? t[j] : -__builtin_inff();
                 if (!named || key >= len) live[j >> 2] &= ~(0xffu << (8 * (j & 3)));
             }

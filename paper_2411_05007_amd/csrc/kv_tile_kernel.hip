@@ -44,8 +44,14 @@ constexpr int tile_lds_bytes(int D, int waves) {
     return tiles > queries ? tiles > out ? tiles : out : queries > out ? queries : out;
 }
 
+struct Hidden {      // keys of a row between the first tokens and its window
+    int from;
+    uint32_t count;
+    __device__ __forceinline__ bool shows(int at) const { return (uint32_t)(at - from) >= count; }
+};
+
 // MORE: with a norm of the queries, or with first tokens that stay visible before a window (else the launch has neither).  Tiles count on without a gap then: first those of the
-// first tokens, then the window's; key_of() and block_of() say where in the sequence that is.
+// first tokens, then the window's, so that a key is less than window_a where it is one of the first tokens', and lies `gap` before its count.
 template <int D, int WAVES, bool MORE>
 __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(KvAttentionParams p) {
     constexpr int C = D / 16, A = D / 32, kRows = 32 * WAVES, kThreads = 64 * WAVES;
@@ -70,7 +76,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     // tiles of keys, and this part's share of them
     const int window_a = wg_lo / kTileKeys * kTileKeys;      // the window's first tile
     const int sinks = MORE ? p.sinks : 0, sink_keys = (int)(((long long)sinks + kTileKeys - 1) / kTileKeys * kTileKeys), gap = MORE ? window_a - (sink_keys < window_a ? sink_keys : window_a) : 0;
-    const auto key_of = [&](int key) { return MORE && key < window_a ? key - gap : key; };
+    const auto hidden_of = [&](int lo) { return Hidden{sinks < lo ? sinks : lo, (uint32_t)(sinks < lo ? lo - sinks : 0)}; };
     const auto block_of = [&](int blk) { return MORE && blk < window_a >> 5 ? blk - (gap >> 5) : blk; };
     const int key_a = MORE ? gap : window_a, tiles_a = wg_hi > window_a ? (wg_hi - key_a + kTileKeys - 1) / kTileKeys : 0;
     const int tile0 = (int)((long long)tiles_a * part / p.parts), tiles_k = (int)((long long)tiles_a * (part + 1) / p.parts) - tile0;
@@ -137,7 +143,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         if (decltype(partial)::value) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (key_of(key0 + t * kTileKeys) + 32 * blk + kv_slot_token(g) + (j & 3) + 8 * (j >> 2) >= len) live[j >> 2] &= ~(0xffu << (8 * (j & 3)));
+                if (key0 + t * kTileKeys + 32 * blk + kv_slot_token(g) + (j & 3) + 8 * (j >> 2) >= len) live[j >> 2] &= ~(0xffu << (8 * (j & 3)));
         }
         unsigned char *dst = vt + ((blk * A + a) * 4 + g) * kSlotBytes + d16 * 16;
         *reinterpret_cast<kv_f16x8 *>(dst) = kv_f16_of(w[i].x & live[0], w[i].y & live[1], vf);
@@ -157,7 +163,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     // LDS as operands. ----
     kv_f16x8 qf[C];
     float to_t = 0.f;      // score -> exponent of 2, but for the block's scale; not negative: a negative scale turns the queries' sign
-    constexpr int U = D / 16, PER = U < 8 || MORE ? 2 : 4;      // units of a row, of a lane at a time (with weights of a norm beside them: fewer)
+    constexpr int U = D / 16, PER = U < 8 ? U / 2 : 4;      // units of a row, of a lane at a time
     constexpr int kChunk = 33 * 16;         // bytes of a run of eight channels of 32 rows in LDS
     unsigned char *my_queries = lds + wave * (2 * U * kChunk + 128);
     float *factors = reinterpret_cast<float *>(my_queries + 2 * U * kChunk);
@@ -166,6 +172,16 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         look_up_bytes(0);
     } else {
         const int half = p.rope.dims / 2;
+        // weights of the norm: a lane's channels are the same in all rows, and so are the weights, but for those of each head and of first tokens that end within the rows
+        const bool one_row = MORE && p.norm.head_stride == 0 && (w_first >= p.norm.first_tokens || w_last < p.norm.first_tokens);
+        const auto weights_at = [&](int pr, int pos, int qh, float (&w)[2][8]) {
+            const bool halves = !p.rope.interleaved && pr < p.rope.dims / 16;
+            const float *row = kv_norm_row(p.norm, pos, qh);
+            kv_load_weights(row, halves ? pr * 8 : pr * 16, w[0]);
+            kv_load_weights(row, halves ? pr * 8 + half : pr * 16 + 8, w[1]);
+        };
+        float weight[2][8];
+        if (MORE && p.norm.on && one_row) weights_at(lane % U, w_first, 0, weight);
         for (int i0 = 0; i0 < U / 2; i0 += PER) {
             uint4 own[PER][2];
             float4 c[PER][2], s[PER][2];
@@ -198,11 +214,8 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
                 kv_floats(own[i][1], x[1]);
                 if (MORE && p.norm.on) {
                     const int r = row0 + wave * 32 + row < rows ? row0 + wave * 32 + row : rows - 1;
-                    const float *weights = kv_norm_row(p.norm, len - n + r / p.group, head * p.group + r % p.group);
-                    float w[2][8];
-                    kv_load_weights(weights, halves ? pr * 8 : pr * 16, w[0]);
-                    kv_load_weights(weights, halves ? pr * 8 + half : pr * 16 + 8, w[1]);
-                    kv_normalise<U>(x, w, p.norm.eps);
+                    if (!one_row) weights_at(pr, len - n + r / p.group, head * p.group + r % p.group, weight);
+                    kv_normalise<U>(x, weight, p.norm.eps);
                 }
                 const float cc[8] = {c[i][0].x, c[i][0].y, c[i][0].z, c[i][0].w, c[i][1].x, c[i][1].y, c[i][1].z, c[i][1].w};
                 const float ss[8] = {s[i][0].x, s[i][0].y, s[i][0].z, s[i][0].w, s[i][1].x, s[i][1].y, s[i][1].z, s[i][1].w};
@@ -285,16 +298,30 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
     };
     // masks the scores of tile t and renews the maximum if they pass it; top: largest(s)
     auto look_at = [&](Scores &s, float (&top)[2], const Facts &f, int t) {
-        const int key = key_of(key0 + t * kTileKeys);
+        const int key = key0 + t * kTileKeys;      // (less than all_lo before the window)
         if (!named(f) || key < all_lo || key + kTileKeys > all_hi) {
             const int pos = pos_of(row0 + wave * 32 + l32), seen_hi = hi_of(pos) < len ? hi_of(pos) : len, seen_lo = lo_of(pos);
+            if (MORE) {      // (no branch for each score: a block that does not exist ends the row's keys before it)
+                const int real = key < window_a ? key - gap : key, first = real + 4 * h32;
+                const Hidden hidden = hidden_of(seen_lo);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 2; ++i) {
+                    const int end = f.unit[i] != -1 ? seen_hi : -1;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int at = key + 32 * i + 8 * (v >> 2) + 4 * h32 + (v & 3);
-                    s[i][v] = f.unit[i] != -1 && (at >= seen_lo || (MORE && at < sinks)) && at < seen_hi ? s[i][v] : -__builtin_inff();
+                    for (int v = 0; v < 16; ++v) {
+                        const int at = first + 32 * i + 8 * (v >> 2) + (v & 3);
+                        s[i][v] = (int)hidden.shows(at) & (int)(at < end) ? s[i][v] : -__builtin_inff();
+                    }
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int at = key + 32 * i + 8 * (v >> 2) + 4 * h32 + (v & 3);
+                        s[i][v] = f.unit[i] != -1 && at >= seen_lo && at < seen_hi ? s[i][v] : -__builtin_inff();
+                    }
+            }
             largest(s, top);
         }
 #pragma unroll
@@ -488,6 +515,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
         l = 0.f;
         row_ref = 0;
         const int pos = pos_of(row0 + wave * 32 + l32), seen_hi = hi_of(pos) < len ? hi_of(pos) : len, seen_lo = lo_of(pos);
+        const Hidden hidden = hidden_of(seen_lo);
         for (int v_blk = blk0; v_blk < blk1; ++v_blk) {
             const int blk = block_of(v_blk);
             const long long unit = kv_unit(p.cache, p.batch.table, p.batch.table_width, b, head, blk);
@@ -504,7 +532,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_tile_kernel(Kv
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int at = blk * kKvBlock + 8 * (i >> 2) + 4 * h32 + (i & 3);
-                s[i] = (at >= seen_lo || (MORE && at < sinks)) && at < seen_hi ? s[i] * f : -__builtin_inff();
+                s[i] = (MORE ? hidden.shows(at) : at >= seen_lo) && at < seen_hi ? s[i] * f : -__builtin_inff();
                 top = fmaxf(top, s[i]);
             }
             top = kv_max32(top);
