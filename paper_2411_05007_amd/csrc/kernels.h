@@ -246,6 +246,8 @@ struct KvCompactParams {
     uint8_t *stage;          // null, or [item][head] blocks: 32 dim codes of keys, of values
     uint8_t *stage_bytes;    // [item][head][2]
 };
+// blocks of the new place that moves may touch
+inline size_t kv_compact_items(int moves, int sequences) { return (size_t)moves / 32 + 2 * (size_t)sequences; }
 hipError_t launch_kv_compact(const KvCompactParams &p, hipStream_t stream);
 struct KvPool {
     int32_t *refs;           // [pages]: table entries that name the page

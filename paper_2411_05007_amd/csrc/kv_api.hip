@@ -148,7 +148,7 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
     // (keys that a row sees: whole blocks of the first ones, where a window is)
     const long long wide = causal ? (long long)window + ((sinks + 31) & ~31) : 0;
     const svdq::KvPlan plan = svdq::plan_kv_attention(batch->sequences, s.kv_heads, q_heads / s.kv_heads, s.head_dim, batch->max_new, batch->max_len,
-                                                      wide > 0x7fffffffll ? 0x7fffffff : (int)wide, batch->new_tokens);
+                                                      wide > 0x7fffffffll ? 0x7fffffff : (int)wide, batch->new_tokens, norm || sinks > 0);
     if (plan.few && (long long)batch->sequences * plan.row_tiles > kMaxGridY) return SVDQ_EUNSUPPORTED;
     // (the size that the query gives, of which a call with fewer tokens or a window may need less: what is refused does not hang on those)
     if (workspace_bytes < svdq::kv_workspace_bytes(batch->sequences, s.kv_heads, q_heads / s.kv_heads, s.head_dim, batch->max_new, batch->max_len)) return SVDQ_ENOSPACE;
@@ -259,7 +259,7 @@ int svdq_kv_copy_pages(const svdq_kv_cache_dev *to, const svdq_kv_cache_dev *fro
 
 size_t svdq_kv_compact_workspace_bytes(const svdq_kv_shape *shape, int sequences, int moves) {
     if (!shape || check_shape(*shape) != SVDQ_OK || sequences < 0 || moves < 0) return 0;
-    const size_t blocks = ((size_t)moves / 32 + 2 * (size_t)sequences) * shape->kv_heads;
+    const size_t blocks = svdq::kv_compact_items(moves, sequences) * shape->kv_heads;
     return blocks == 0 ? 256 : blocks * 64 * shape->head_dim + (2 * blocks + 255) / 256 * 256;
 }
 
@@ -287,7 +287,7 @@ int svdq_kv_compact(const svdq_kv_cache_dev *to, const svdq_kv_cache_dev *from, 
     p.per_head = moves->per_head != 0;
     p.rope = rope_of(rope);
     p.stage = static_cast<uint8_t *>(workspace);
-    if (workspace) p.stage_bytes = p.stage + ((size_t)moves->moves / 32 + 2 * (size_t)moves->sequences) * to->shape.kv_heads * 64 * to->shape.head_dim;
+    if (workspace) p.stage_bytes = p.stage + svdq::kv_compact_items(moves->moves, moves->sequences) * to->shape.kv_heads * 64 * to->shape.head_dim;
     return done(svdq::launch_kv_compact(p, static_cast<hipStream_t>(hip_stream)));
 }
 

@@ -873,7 +873,8 @@ inline size_t kv_workspace_bytes(int sequences, int heads, int group, int dim, i
 }
 // tokens: new ones of all sequences, -1 if they are not known yet (the workspace for any number of them).  window: 0 or the keys that a row sees.  Neither changes
 // the kernel of the longest sequence, and a call needs no more workspace than without them.
-inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len, int window, long long tokens) {
+// wide: a call that may take the larger tiles in a window too (those that could not before keep their kernel, and so their bits).
+inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, int max_new, int max_len, int window, long long tokens, bool wide = false) {
     KvPlan p{};
     const long long rows = (long long)max_new * group, most_tokens = (long long)sequences * max_new;
     p.few = kv_few_rows(sequences, heads, dim, rows, max_len);
@@ -886,9 +887,10 @@ inline KvPlan plan_kv_attention(int sequences, int heads, int group, int dim, in
     }
     // 256 rows, one workgroup on a CU, stage a tile of keys for twice the rows: 8192 tokens x 4 heads on 16384 keys 1530 us (128 rows: 1618), joint attention of 4608
     // tokens 278 (300), whole prompts of 4096 336 (332); what is masked or left over is larger, though: whole prompts of 2048 226 (212), ragged chunks 357 (355), 7409
-    // rows x 2 in a window 498 (469).
+    // rows x 2 in a window 498 (469).  In a window the keys that only some of a tile's tokens see count, so it is to be 32 times as long as those (256 / group): 8192 tokens x 4
+    // heads in a window of 8192 on 24576 keys 1092 us (1150), of 4096 574 (600), of 1024 200 (202); 2048 in 8192 290 (317); 4096 x 2 in 2048 677 (671), 4608 x 1 in 4096 290 (291).
     const long long slots = dim == 256 ? 256 : 512, large = (long long)sequences * ((rows + 255) / 256) * heads;
-    p.tile_rows = dim == 128 && tokens == most_tokens && window == 0 && max_len >= 4096 && large >= 256 ? 256 : 128;
+    p.tile_rows = dim == 128 && tokens == most_tokens && (window == 0 || (wide && (long long)window * group >= 32 * 256)) && max_len >= 4096 && large >= 256 ? 256 : 128;
     const long long keys = window > 0 && (long long)window + 128 / group < max_len ? (long long)window + 128 / group : max_len;
     // Does the batch hold chunks beside single tokens?  Where the mean sequence has less than a third of the most tokens, or all but one have sixteen rows in the mean.
     const bool mixed = sequences > 1 && group <= kKvFewRows && (10 * tokens < 3 * most_tokens || (tokens - max_new) * group <= (long long)kKvFewRows * (sequences - 1));

@@ -282,6 +282,29 @@ def test_the_first_tokens_stay_visible(torch, KV, dim, heads, group, page, held,
     w.attend(x, xn, new, window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("sequences,heads,group,held,new,window,sinks,norm", [
+    (4, 8, 4, 3700, 512, 2100, 70, dict(first=100)),        # row tiles of 256 (tests/test_kv_stream_plan.py has the rule)
+    (32, 8, 1, 3900, 256, 0, 0, dict(per_head=True)),
+    (32, 4, 2, 3968, 130, 4096, 1, None),
+])
+def test_the_larger_tiles(torch, KV, sequences, heads, group, held, new, window, sinks, norm):
+    w = Stream(torch, KV, heads, 128, 128, [held + new] * sequences, 70 + sequences, q_heads=heads * group, dims=128, norm=norm)
+    w.append([held] * sequences)
+    x, xn, _ = w.append([new] * sequences)
+    got = w.attend(x[:new], xn[:new], [new] + [0] * (sequences - 1), window=window, sinks=sinks)      # alone: row tiles of 128
+    batch, cu = w.batch([new] * sequences)
+    out = w.cache.attention(x[:, :heads * group], batch, w.rope, window=window, sinks=sinks, norm=w.norm.dev if norm is not None else None).float().cpu().numpy()
+    assert np.abs(out[:new] - got).max() <= 2.0 ** -7 * np.abs(got).max()
+    for b in (1, sequences - 1):
+        at, part = held + np.arange(new), slice(cu[b], cu[b + 1])
+        k, v, _, _ = w.rows(b)
+        some = np.unique(np.concatenate([np.arange(0, new, 37), [new - 1]]))      # (rows of all wavefronts)
+        q = xn[part, :heads * group][some]
+        q, size = w.norm.ready(q, at[some], "q", w.rope_np, False) if norm is not None else W.turn(q.astype(np.float64), at[some], w.rope_np, False)
+        want, tol = W.attention(q, size, k, v, at[some], np.arange(held + new), 128 ** -0.5, True, window, sinks)
+        assert (np.abs(out[part][some] - want) <= tol).all(), b
+
+
 @pytest.mark.parametrize("dim,new,group", [(128, 1, 4), (128, 90, 4), (64, 2, 2), (64, 200, 1), (256, 1, 1), (256, 90, 2)])
 def test_first_tokens_of_other_scales(torch, KV, dim, new, group):
     """Blocks of very different scales: those of the first tokens and of the window meet a block at a time, and what no row sees leaves no trace."""
