@@ -25,6 +25,12 @@ constexpr int kStages = 4;          // old blocks in LDS at a time
 constexpr int kStageRow = 80;       // bytes apart of rows of 64
 template <int D> constexpr int kStageBytes = D / 32 * 16 * kStageRow;
 
+template <int D> struct Shelf {      // the old blocks of values in LDS, and how a token is found there
+    __attribute__((aligned(16))) unsigned char blocks[kStages * kStageBytes<D>];
+    uint32_t spot[kKvBlock];
+    float scale[kKvBlock];
+};
+
 struct Place { BlockWork w; int sequence; };
 // The new place's block of a work item; w.lo >= w.hi: none.  row0: the move that its token 0 would be.
 __device__ __forceinline__ Place place_of(const KvCompactParams &p, int number) {
@@ -126,40 +132,45 @@ struct KeyMoves {
             stays[i] = from == to;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float m = __builtin_amdgcn_rcpf(c0[e] * c0[e] + s0[e] * s0[e]);
-                c[i][e] = (c1[e] * c0[e] + s1[e] * s0[e]) * m;
-                s[i][e] = (s1[e] * c0[e] - c1[e] * s0[e]) * m;
+                const float size = __builtin_fmaf(c0[e], c0[e], s0[e] * s0[e]), near = __builtin_amdgcn_rcpf(size);
+                const float m = __builtin_fmaf(__builtin_fmaf(-size, near, 1.f), near, near);      // 1 / size, a step of Newton's on the instruction's
+                c[i][e] = __builtin_fmaf(c1[e], c0[e], s1[e] * s0[e]) * m;
+                s[i][e] = __builtin_fmaf(s1[e], c0[e], -(c1[e] * s0[e])) * m;
             }
         }
     }
-    __device__ __forceinline__ void gather(const Sources &src, int, unsigned char *, int runs) {
+    __device__ __forceinline__ void gather(const Sources &, int, int, Shelf<D> &, int runs) {
         for (int done = 0; done < runs; done += kStages) {      // (the values' wavefronts do)
             if (done > 0) kv_lds_barrier();
             kv_lds_barrier();
         }
     }
-    // turns the rows; returns the tokens with an element that is not finite
-    __device__ __forceinline__ uint32_t look() {
+    // turns the rows; returns the tokens with an element that is not finite.  Asks for the rows of head `next`, if there is one
+    __device__ __forceinline__ uint32_t look(const Sources &src, int next) {
         uint32_t bad = 0u;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float scale = byte_scale(byte[i]);
             code_numbers(raw[i][0], scale, x[i][0]);
             code_numbers(raw[i][1], scale, x[i][1]);
+        }
+        if (next >= 0) load(src, next);      // (its rows are in flight while this head's are worked on)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
             if (lane % U < p.rope.dims / 16 && !stays[i]) {
                 if (p.rope.interleaved) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float a = x[i][e / 4][2 * (e % 4)], y = x[i][e / 4][2 * (e % 4) + 1];
-                        x[i][e / 4][2 * (e % 4)] = kv_turn_a(a, y, c[i][e], s[i][e]);
-                        x[i][e / 4][2 * (e % 4) + 1] = kv_turn_b(a, y, c[i][e], s[i][e]);
+                        x[i][e / 4][2 * (e % 4)] = kv_turn_fma_a(a, y, c[i][e], s[i][e]);
+                        x[i][e / 4][2 * (e % 4) + 1] = kv_turn_fma_b(a, y, c[i][e], s[i][e]);
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float a = x[i][0][e], y = x[i][1][e];
-                        x[i][0][e] = kv_turn_a(a, y, c[i][e], s[i][e]);
-                        x[i][1][e] = kv_turn_b(a, y, c[i][e], s[i][e]);
+                        x[i][0][e] = kv_turn_fma_a(a, y, c[i][e], s[i][e]);
+                        x[i][1][e] = kv_turn_fma_b(a, y, c[i][e], s[i][e]);
                     }
                 }
             }
@@ -207,68 +218,93 @@ struct ValueMoves {
     const KvCompactParams &p;
     const Place &at;
     const int lane, half;
-    uint4 staged[kStages][N];
+    kv_u32x4 staged[kStages][N];
     float x[N][2][8], top[8];
     int byte_l;                  // of the lane's token
     __device__ __forceinline__ int token(int j) const { return kv_slot_token(lane & 3) + (j & 3) + 8 * (j >> 2); }
     __device__ __forceinline__ int piece(int i) const { return lane + 64 * half + 128 * i; }
     __device__ __forceinline__ ValueMoves(const KvCompactParams &p_, const Place &at_, int lane_, int half_) : p(p_), at(at_), lane(lane_), half(half_) {}
-    __device__ __forceinline__ void load_runs(const Sources &src, int h, int first, int runs, unsigned long long starts) {
+    __device__ __forceinline__ void load_runs(const Sources &src, int h, int first, unsigned long long starts) {      // up to kStages of them, from the first-th on
+        for (int n = 0; n < first; ++n) starts &= starts - 1;
+        size_t unit[kStages];
+        bool some[kStages];
 #pragma unroll
         for (int k = 0; k < kStages; ++k) {
-            if (first + k >= runs) break;
-            unsigned long long left = starts;
-            for (int n = 0; n < first + k; ++n) left &= left - 1;
-            const uint32_t u0 = (uint32_t)__builtin_amdgcn_readlane((int)src.unit, __builtin_ctzll(left));
-            const uint8_t *block = p.from.v + (u0 == ~0u ? 0 : (size_t)u0 + ((size_t)h << (p.from.page_shift - 5))) * (32 * D);
-#pragma unroll
-            for (int i = 0; i < N; ++i) staged[k][i] = *reinterpret_cast<const uint4 *>(block + piece(i) * 16);
+            some[k] = starts != 0ull;
+            const uint32_t u0 = (uint32_t)__builtin_amdgcn_readlane((int)src.unit, some[k] ? __builtin_ctzll(starts) : 0);
+            unit[k] = u0 == ~0u ? 0 : (size_t)u0 + ((size_t)h << (p.from.page_shift - 5));
+            starts &= starts - 1;
         }
+#pragma unroll
+        for (int k = 0; k < kStages; ++k)
+            if (some[k]) {
+                const uint8_t *block = p.from.v + unit[k] * (32 * D);
+#pragma unroll
+                for (int i = 0; i < N; ++i) staged[k][i] = *reinterpret_cast<const kv_u32x4 *>(block + piece(i) * 16);
+            }
     }
     __device__ __forceinline__ void load(const Sources &src, int h) {
         byte_l = p.from.vs[src.of_head(p, h)];
         int mine;
         unsigned long long starts;
-        const int runs = src.runs(lane, mine, starts);
-        load_runs(src, h, 0, runs, starts);
+        src.runs(lane, mine, starts);
+        load_runs(src, h, 0, starts);
     }
     __device__ __forceinline__ void angles(const Sources &) {}
-    __device__ __forceinline__ void gather(const Sources &src, int h, unsigned char *lds, int runs) {
+    __device__ __forceinline__ void gather(const Sources &src, int h, int next, Shelf<D> &shelf, int runs) {
         int mine;
         unsigned long long starts;
         src.runs(lane, mine, starts);
-        const int t = src.token & 31;      // place of the lane's token in its old block: slot and byte of the slot
-        const int spot = (2 * (t / 16) + t % 8 / 4) * 16 + 4 * (t % 16 / 8) + t % 4;
+        if (half == 0 && lane < 32) {      // what the token is found by: run, slot and byte of the slot; its scale
+            const int t = src.token & 31;
+            shelf.spot[lane] = (uint32_t)(mine << 8 | ((2 * (t / 16) + t % 8 / 4) * 16 + 4 * (t % 16 / 8) + t % 4));
+            shelf.scale[lane] = byte_scale(byte_l);
+        }
+        const bool whole = __builtin_amdgcn_ballot_w64(src.unit == ~0u) == 0ull && at.w.lo == 0 && at.w.hi == kKvBlock;      // every token moves
         for (int done = 0; done < runs; done += kStages) {
             if (done > 0) {
-                load_runs(src, h, done, runs, starts);
+                load_runs(src, h, done, starts);
                 kv_lds_barrier();      // (what lay there is picked)
             }
 #pragma unroll
             for (int k = 0; k < kStages; ++k) {
-                if (done + k >= runs) break;
+                if (done + k >= runs) continue;
 #pragma unroll
-                for (int i = 0; i < N; ++i) *reinterpret_cast<uint4 *>(lds + k * kStageBytes<D> + piece(i) / 4 * kStageRow + piece(i) % 4 * 16) = staged[k][i];
+                for (int i = 0; i < N; ++i) *reinterpret_cast<kv_u32x4 *>(shelf.blocks + k * kStageBytes<D> + piece(i) / 4 * kStageRow + piece(i) % 4 * 16) = staged[k][i];
             }
+            if (next >= 0 && done + kStages >= runs) load(src, next);      // (in flight while this head's are picked)
             kv_lds_barrier();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int run = __shfl(mine, token(j)) - done, from = __shfl(spot, token(j)), byte = __shfl(byte_l, token(j));
-                const bool named = __shfl((int)src.unit, token(j)) != -1;
-                if (run < 0 || run >= kStages) continue;
-                const unsigned char *tok = lds + run * kStageBytes<D> + from;
-                const bool moves = live(at.w, token(j)) && named;
-                const float scale = byte_scale(byte);
+            for (int j0 = 0; j0 < 8; j0 += 4) {
+                const uint4 spots = *reinterpret_cast<const uint4 *>(shelf.spot + token(j0));
+                const float4 scales = *reinterpret_cast<const float4 *>(shelf.scale + token(j0));
+                const uint32_t spot[4] = {spots.x, spots.y, spots.z, spots.w};
+                const float scale[4] = {scales.x, scales.y, scales.z, scales.w};
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float a = code_number(tok[piece(i) / 4 * kStageRow], scale), b = code_number(tok[piece(i) / 4 * kStageRow + 8], scale);
-                    x[i][0][j] = moves ? a : 0.f;
-                    x[i][1][j] = moves ? b : 0.f;
+                for (int j = 0; j < 4; ++j) {
+                    const int run = (int)(spot[j] >> 8) - done;
+                    if (runs > kStages && (run < 0 || run >= kStages)) continue;
+                    const unsigned char *tok = shelf.blocks + run * kStageBytes<D> + (spot[j] & 255u) + lane / 4 * kStageRow + half * (16 * kStageRow);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        x[i][0][j0 + j] = code_number(tok[i * (32 * kStageRow)], scale[j]);
+                        x[i][1][j0 + j] = code_number(tok[i * (32 * kStageRow) + 8], scale[j]);
+                    }
                 }
             }
         }
+        if (whole) return;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool moves = live(at.w, token(j)) && __shfl((int)src.unit, token(j)) != -1;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                x[i][0][j] = moves ? x[i][0][j] : 0.f;
+                x[i][1][j] = moves ? x[i][1][j] : 0.f;
+            }
+        }
     }
-    __device__ __forceinline__ uint32_t look() {
+    __device__ __forceinline__ uint32_t look(const Sources &, int) {
         float all = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -318,7 +354,7 @@ struct ValueMoves {
 };
 
 template <int D, typename Side>
-__device__ __forceinline__ void compact_heads(const KvCompactParams &p, const Place &at, int h0, int h1, int wave, unsigned char *lds, Exchange (&exchange)[2]) {
+__device__ __forceinline__ void compact_heads(const KvCompactParams &p, const Place &at, int number, int h0, int h1, int wave, Shelf<D> &shelf, Exchange (&exchange)[2]) {
     const bool keys = wave < 2;
     const int lane = threadIdx.x & 63;
     Side side(p, at, lane, wave & 1);
@@ -333,7 +369,7 @@ __device__ __forceinline__ void compact_heads(const KvCompactParams &p, const Pl
         uint8_t *codes = (keys ? p.to.k : p.to.v) + (size_t)unit * (32 * D), *byte = (keys ? p.to.ks : p.to.vs) + unit;
         Target to = {codes, byte, codes};
         if (p.stage) {
-            const size_t slot = (size_t)blockIdx.x * p.to.heads + h;
+            const size_t slot = (size_t)number * p.to.heads + h;
             to.codes = p.stage + (2 * slot + (keys ? 0 : 1)) * (32 * D);
             to.byte = p.stage_bytes + 2 * slot + (keys ? 0 : 1);
         }
@@ -341,9 +377,10 @@ __device__ __forceinline__ void compact_heads(const KvCompactParams &p, const Pl
         const int held = tells && at.w.lo > 0 ? (int)*byte : 0;
         int mine;
         unsigned long long starts;
-        side.gather(src, h, lds, src.runs(lane, mine, starts));
+        const int next = h + 1 < h1 ? h + 1 : -1;
+        side.gather(src, h, next, shelf, src.runs(lane, mine, starts));
         Exchange &ex = exchange[h & 1];      // (written again two heads on: behind a barrier that every wavefront enters when it has read it)
-        const uint32_t bad = side.look(), most = side.largest(bad);
+        const uint32_t bad = side.look(src, next), most = side.largest(bad);
         if (lane == 0) {
             ex.bad[wave] = bad;
             ex.top[wave] = most;
@@ -360,20 +397,20 @@ __device__ __forceinline__ void compact_heads(const KvCompactParams &p, const Pl
         const BlockScale sc = block_scale(umax(ex.top[wave & 2], ex.top[(wave & 2) + 1]), __builtin_amdgcn_readfirstlane(ex.old_byte[wave >> 1]));
         side.write(to, sc, all);
         if (tells) *to.byte = (uint8_t)sc.byte;
-        if (h + 1 < h1) side.load(src, h + 1);      // (tokens of each head's own: one head a workgroup)
     }
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void kv_compact_kernel(KvCompactParams p, int heads_per_wg) {
+__global__ __launch_bounds__(256, D > 128 ? 2 : D > 64 ? 4 : 5) void kv_compact_kernel(KvCompactParams p, int heads_per_wg) {
     __shared__ Exchange exchange[2];
-    __shared__ __attribute__((aligned(16))) unsigned char lds[kStages * kStageBytes<D>];
-    const Place at = place_of(p, blockIdx.x);
+    __shared__ Shelf<D> shelf;
+    const int number = blockIdx.x;
+    const Place at = place_of(p, number);
     if (at.w.lo >= at.w.hi) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h0 = blockIdx.y * heads_per_wg, h1 = h0 + heads_per_wg < p.to.heads ? h0 + heads_per_wg : p.to.heads;
-    if (wave < 2) compact_heads<D, KeyMoves<D>>(p, at, h0, h1, wave, lds, exchange);
-    else compact_heads<D, ValueMoves<D>>(p, at, h0, h1, wave, lds, exchange);
+    if (wave < 2) compact_heads<D, KeyMoves<D>>(p, at, number, h0, h1, wave, shelf, exchange);
+    else compact_heads<D, ValueMoves<D>>(p, at, number, h0, h1, wave, shelf, exchange);
 }
 
 // Puts the blocks of the workspace in place.
@@ -395,9 +432,11 @@ __global__ __launch_bounds__(128) void kv_place_kernel(KvCompactParams p) {
 
 template <int D>
 hipError_t launch_compact(const KvCompactParams &p, hipStream_t stream) {
-    const int items = p.batch.total / kKvBlock + 2 * p.batch.sequences;
+    const int items = (int)kv_compact_items(p.batch.total, p.batch.sequences);
+    // Heads a workgroup, where one list serves all: as many as leave workgroups for one round of the chip (256 CUs, four each), up to eight, so that tokens, pages and angles are looked
+    // up once.  1.1 million tokens of eight heads of 128, two thirds of them kept: 762 us with two, 663 with four, 621 with eight.
     const long long rounds = (long long)items * p.to.heads / 1024;
-    const int most = p.per_head || rounds < 1 ? 1 : rounds > 4 ? 4 : (int)rounds, per = most < p.to.heads ? most : p.to.heads;
+    const int most = p.per_head || rounds < 1 ? 1 : rounds > 8 ? 8 : (int)rounds, per = most < p.to.heads ? most : p.to.heads;
     kv_compact_kernel<D><<<dim3(items, (p.to.heads + per - 1) / per), 256, 0, stream>>>(p, per);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.stage) return e;
