@@ -8,7 +8,7 @@
 //   copy      pages of one cache into pages of the same or another one
 // Reserve is two kernels.  The first notes what is free (a bit a page, counts for each 1024) and which entries lack a page (a bit an entry, a count for each sequence), the second
 // sums what comes before its sequence, enumerates the free pages from there and the entries side by side through LDS, and writes table and counts; further workgroups of the
-// sequence copy.  Decisions are made from the first one's notes alone, so the order in which workgroups change tables and counts does not matter.
+// sequence find the one page that they copy to by themselves.  Decisions are made from the first one's notes alone, so the order in which workgroups change tables and counts does not matter.
 // Bound: latency, of two launches; then memory, for the copies.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -22,10 +22,10 @@ namespace {
 __device__ __forceinline__ bool is_page(int page, int pages) { return (uint32_t)page < (uint32_t)pages; }
 __device__ __forceinline__ void count_by(int32_t *refs, int by) { (void)__hip_atomic_fetch_add(refs, by, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-__global__ __launch_bounds__(256) void kv_release_kernel(KvPool pool, int32_t *table, const int32_t *first, const int32_t *last, int sequences, int width) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (long long)sequences * width) return;
-    const int b = (int)(i / width), e = (int)(i % width);
+__global__ __launch_bounds__(256) void kv_release_kernel(KvPool pool, int32_t *table, const int32_t *first, const int32_t *last, int width) {
+    const int b = blockIdx.y, e = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (e >= width) return;
+    const size_t i = (size_t)b * width + e;
     const long long lo = first ? first[b] : 0, hi = last ? (long long)last[b] : 1ll << 62;
     if (((long long)e << pool.page_shift) < lo || ((long long)(e + 1) << pool.page_shift) > hi) return;
     const int page = table[i];
@@ -34,9 +34,9 @@ __global__ __launch_bounds__(256) void kv_release_kernel(KvPool pool, int32_t *t
 }
 
 __global__ __launch_bounds__(256) void kv_fork_kernel(KvForkParams p) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (long long)p.sequences * p.to_width) return;
-    const int b = (int)(i / p.to_width), e = (int)(i % p.to_width), from = p.parent[b];
+    const int b = blockIdx.y, e = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (e >= p.to_width) return;
+    const int from = p.parent[b];
     int len = 0, page = -1;
     if ((uint32_t)from < (uint32_t)p.from_sequences) {
         const long long most = (long long)(p.from_width < p.to_width ? p.from_width : p.to_width) << p.pool.page_shift;
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void kv_fork_kernel(KvForkParams p) {
     }
     if (!is_page(page, p.pool.pages)) page = -1;
     else count_by(p.pool.refs + page, 1);
-    p.to_table[i] = page;
+    p.to_table[(size_t)b * p.to_width + e] = page;
     if (e == 0) p.to_len[b] = len;
 }
 
@@ -54,10 +54,10 @@ __global__ __launch_bounds__(256) void kv_fork_kernel(KvForkParams p) {
 constexpr int kSlicePages = 1024;      // pages of a count
 struct Entries { int lo, hi, before; };      // of a sequence's table that its new tokens fall in; tokens before them
 __device__ __forceinline__ Entries entries_of(const KvReserveParams &p, int b) {
-    int t0, n;
-    kv_range(p.batch.cu, b, p.batch.total, t0, n);
+    const int cu0 = p.batch.cu[b], cu1 = p.batch.cu[b + 1], kv_len = p.batch.kv_len[b];
+    const int t0 = kv_within(cu0, 0, p.batch.total), n = __builtin_amdgcn_readfirstlane(kv_within(cu1, t0, p.batch.total) - t0);
     const long long most = (long long)p.batch.table_width << p.pool.page_shift;
-    int len = __builtin_amdgcn_readfirstlane(p.batch.kv_len[b]);
+    int len = __builtin_amdgcn_readfirstlane(kv_len);
     len = len < 0 ? 0 : (long long)len > most ? (int)most : len;
     const int before = len > n ? len - n : 0;
     Entries e = {before >> p.pool.page_shift, (int)(((long long)len + (1 << p.pool.page_shift) - 1) >> p.pool.page_shift), before};
@@ -112,33 +112,24 @@ __global__ __launch_bounds__(256) void kv_reserve_plan_kernel(KvReserveParams p)
     }
 }
 
-// Copies the blocks of a page's first tokens, part `part` of `parts` of it (a workgroup of 256).
+// Copies the blocks of a page's first tokens, part `part` of `parts` of it (a workgroup of 256): the keys and values of a head lie in a row, and go in chunks of 16 KB.
 __device__ __forceinline__ void copy_page(const KvCache &to, const KvCache &from, int to_page, int from_page, int tokens, int part, int parts) {
     const int bs = to.page_shift - 5, most = 1 << bs, blocks = (tokens + 31) >> 5 < most ? (tokens + 31) >> 5 : most;
     if (blocks <= 0) return;
-    const int per = blocks * 2 * to.dim, total = to.heads * 2 * per;      // pieces of 16 bytes of a head's keys or values, of all
+    constexpr int kAhead = 4, kChunk = 256 * kAhead;
+    const int pieces = blocks * 2 * to.dim, chunks = (pieces + kChunk - 1) / kChunk, items = to.heads * 2 * chunks;      // pieces of 16 bytes of a head's keys, or values
     const size_t to_unit = ((size_t)to_page * to.heads) << bs, from_unit = ((size_t)from_page * to.heads) << bs;
-    const auto src = [&](int i) {
-        const int side = i / per, h = side >> 1;
-        return reinterpret_cast<const uint4 *>((side & 1 ? from.v : from.k) + (from_unit + ((size_t)h << bs)) * (32 * (size_t)to.dim)) + i % per;
-    };
-    const auto dst = [&](int i) {
-        const int side = i / per, h = side >> 1;
-        return reinterpret_cast<uint4 *>((side & 1 ? to.v : to.k) + (to_unit + ((size_t)h << bs)) * (32 * (size_t)to.dim)) + i % per;
-    };
-    constexpr int kAhead = 4;
-    for (int i0 = part * 256 * kAhead; i0 < total; i0 += parts * 256 * kAhead) {
-        uint4 w[kAhead];
+    for (int item = part; item < items; item += parts) {
+        const int side = item / chunks, at = item % chunks * kChunk + (int)threadIdx.x;
+        const size_t head = (size_t)(side >> 1) << bs;
+        const kv_u32x4 *src = reinterpret_cast<const kv_u32x4 *>((side & 1 ? from.v : from.k) + (from_unit + head) * (32 * (size_t)to.dim));
+        kv_u32x4 *dst = reinterpret_cast<kv_u32x4 *>((side & 1 ? to.v : to.k) + (to_unit + head) * (32 * (size_t)to.dim));
+        kv_u32x4 w[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int i = i0 + 256 * k + threadIdx.x;
-            w[k] = *src(i < total ? i : total - 1);
-        }
+        for (int k = 0; k < kAhead; ++k) w[k] = src[at + 256 * k < pieces ? at + 256 * k : pieces - 1];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int i = i0 + 256 * k + threadIdx.x;
-            if (i < total) *dst(i) = w[k];
-        }
+        for (int k = 0; k < kAhead; ++k)
+            if (at + 256 * k < pieces) dst[at + 256 * k] = w[k];
     }
     if (part == 0)
         for (int i = threadIdx.x; i < to.heads * blocks; i += 256) {
@@ -148,108 +139,121 @@ __device__ __forceinline__ void copy_page(const KvCache &to, const KvCache &from
         }
 }
 
-// Free pages in order, from the `skip`-th on, up to `most` of them into `out` (a wavefront); returns how many there were.
-__device__ __forceinline__ int free_pages(const KvReserveParams &p, int skip, int most, int *out) {
-    const int lane = threadIdx.x & 63;
-    int s0 = 0, got = 0;
-    for (; s0 < p.slices; s0 += 64) {      // the slice that has it
-        const int mine = s0 + lane < p.slices ? p.slice_free[s0 + lane] : 0, upto = kv_sum_upto(mine);
-        const unsigned long long past = __builtin_amdgcn_ballot_w64(upto > skip);
-        if (past != 0ull) {
-            const int at = __builtin_ctzll(past);
-            skip -= __builtin_amdgcn_readlane(upto - mine, at);
-            s0 += at;
-            break;
-        }
-        skip -= __builtin_amdgcn_readlane(upto, 63);
+// What a wavefront of a sequence needs of the first kernel's notes, asked for at once: the entries that lack a page in sequences before `b`, the free pages of the first 64 slices (one in
+// a lane) and the first 64 words of their bits.
+struct Notes {
+    int before, slice_l;
+    unsigned long long word_l;
+    __device__ __forceinline__ void read(const KvReserveParams &p, int b) {
+        const int lane = threadIdx.x & 63;
+        slice_l = lane < p.slices ? p.slice_free[lane] : 0;
+        word_l = p.free_words[lane < p.slices * (kSlicePages / 64) ? lane : 0];
+        int sum = 0;
+#pragma unroll 4
+        for (int i = lane; i < b; i += 64) sum += p.lack_count[i];
+        before = wave_sum(sum);
     }
-    const int words = p.slices * (kSlicePages / 64);
-    for (int w0 = s0 * (kSlicePages / 64); w0 < words && got < most; w0 += 64) {      // 64 words at a time
-        const unsigned long long word = w0 + lane < words ? p.free_words[w0 + lane] : 0ull;
-        const int here = __builtin_popcountll(word), upto = kv_sum_upto(here), total = __builtin_amdgcn_readlane(upto, 63);
-        // the lane's pages have the numbers upto - here .. upto - 1; those from `skip` on are taken
-        int number = upto - here - skip + got;
-        for (unsigned long long left = word; left != 0ull && number < most; left &= left - 1, ++number)
-            if (number >= got) out[number] = (w0 + lane) * 64 + __builtin_ctzll(left);
-        const int taken = total > skip ? total - skip : 0;
-        got = got + taken < most ? got + taken : most;
+};
+// Free pages in order, from the `skip`-th on, up to `most` of them into `out`; returns how many there were.
+__device__ __forceinline__ int free_pages(const KvReserveParams &p, const Notes &notes, int skip, int most, int *out) {
+    const int lane = threadIdx.x & 63, words = p.slices * (kSlicePages / 64);
+    int s0 = 0;
+    if (p.slices > 4)
+        for (; s0 < p.slices; s0 += 64) {      // the slice that has it
+            const int mine = s0 == 0 ? notes.slice_l : s0 + lane < p.slices ? p.slice_free[s0 + lane] : 0, upto = kv_sum_upto(mine);
+            const unsigned long long past = __builtin_amdgcn_ballot_w64(upto > skip);
+            if (past != 0ull) {
+                const int at = __builtin_ctzll(past);
+                skip -= __builtin_amdgcn_readlane(upto - mine, at);
+                s0 += at;
+                break;
+            }
+            skip -= __builtin_amdgcn_readlane(upto, 63);
+        }
+    int got = 0;
+    for (int w0 = s0 * (kSlicePages / 64); w0 < words && got < most; w0 += 64) {      // 64 words at a time, one in a lane
+        unsigned long long word = w0 == 0 ? notes.word_l : w0 + lane < words ? p.free_words[w0 + lane] : 0ull;
+        if (w0 + lane >= words) word = 0ull;
+        const int here = __builtin_popcountll(word), upto = kv_sum_upto(here);
+        unsigned long long left = __builtin_amdgcn_ballot_w64(here > 0 && upto > skip);      // words that still matter, one after the other: a page in a lane
+        for (; left != 0ull && got < most; left &= left - 1) {
+            const int at = __builtin_ctzll(left);
+            const unsigned long long bits = ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(word >> 32), at) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)word, at);
+            const int first = __builtin_amdgcn_readlane(upto - here, at), number = first + __builtin_popcountll(bits & ((1ull << lane) - 1ull)) - skip + got;
+            if (((bits >> lane) & 1ull) && number >= got && number < most) out[number] = (w0 + at) * 64 + lane;
+            const int end = first + __builtin_popcountll(bits), taken = end - skip;      // (at least one)
+            got = got + taken < most ? got + taken : most;
+            skip = end;
+        }
+        const int total = __builtin_amdgcn_readlane(upto, 63);
         skip = skip > total ? skip - total : 0;
     }
     return got;
 }
 
+// Part 0 of a sequence writes tables and counts, the others copy.
 __global__ __launch_bounds__(256) void kv_reserve_kernel(KvReserveParams p) {
     constexpr int kRound = 256;
-    __shared__ int pages[kRound], entry[kRound], sums[3][4];
-    __shared__ int found;
+    __shared__ int pages[kRound], entry[kRound], target_of[4], found;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = blockIdx.x, part = blockIdx.y;
-    const bool writes = part == 0, first_of_all = b == 0 && writes;
     const int count = p.lack_count[b], shared = p.shared[b];
-    if (!first_of_all && (writes ? count == 0 && !p.copies : shared < 0 || !p.cache.k)) return;
-    // entries that lack a page in sequences before this one (and, for one workgroup, in all; and the free pages)
-    int before = 0, all = 0, free = 0;
-    const int last = first_of_all ? p.batch.sequences : b;
-    for (int i = threadIdx.x; i < last; i += 256) {
-        const int n = p.lack_count[i];
-        before += i < b ? n : 0;
-        all += n;
-    }
-    if (first_of_all)
-        for (int i = threadIdx.x; i < p.slices; i += 256) free += p.slice_free[i];
-    before = wave_sum(before);
-    all = wave_sum(all);
-    free = wave_sum(free);
-    if (lane == 0) {
-        sums[0][wave] = before;
-        sums[1][wave] = all;
-        sums[2][wave] = free;
-    }
-    __syncthreads();
-    before = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-    if (first_of_all && threadIdx.x == 0 && p.missing) {
-        const int lack = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3] - (sums[2][0] + sums[2][1] + sums[2][2] + sums[2][3]);
-        *p.missing = lack > 0 ? lack : 0;
-    }
-    if (count == 0) {
-        if (writes && p.copies && threadIdx.x < 3) p.copies[3 * b + threadIdx.x] = threadIdx.x < 2 ? -1 : 0;
+    if (part > 0) {
+        Notes notes;
+        notes.read(p, b);
+        const Entries at = entries_of(p, b);
+        if (shared < 0) return;
+        if (free_pages(p, notes, notes.before, 1, target_of + wave) == 0) return;      // (the same in all wavefronts)
+        __builtin_amdgcn_wave_barrier();
+        const int target = __builtin_amdgcn_readfirstlane(*(volatile int *)(target_of + wave));
+        copy_page(p.cache, p.cache, target, shared, at.before - (at.lo << p.pool.page_shift), part - 1, (int)gridDim.y - 1);
         return;
     }
-    const Entries at = entries_of(p, b);
-    const int held = at.before - (at.lo << p.pool.page_shift);      // tokens of a shared page before the new ones
+    if (b == 0 && wave == 3 && p.missing) {      // entries that lack a page, in all, and free pages
+        int lack = 0;
+        for (int i = lane; i < p.batch.sequences; i += 64) lack += p.lack_count[i];
+        for (int i = lane; i < p.slices; i += 64) lack -= p.slice_free[i];
+        lack = wave_sum(lack);
+        if (lane == 0) *p.missing = lack > 0 ? lack : 0;
+    }
     int target = -1;      // of the copy: the first page
-    for (int done = 0; done < count; done += kRound) {
-        const int round = writes ? (count - done < kRound ? count - done : kRound) : 1;
-        if (wave == 0) {
-            const int n = free_pages(p, before + done, round, pages);
-            if (lane == 0) found = n;
-        } else if (wave == 1 && writes) {      // the entries of this round, from where the last one ended
-            int got = 0, skip = done;
-            for (int e = at.lo & ~63; e < at.hi && got < round; e += 64) {
-                const unsigned long long word = p.lacks[(size_t)b * p.words + (e >> 6)];
-                const int total = __builtin_popcountll(word), number = __builtin_popcountll(word & ((1ull << lane) - 1ull)) - skip + got;
-                if (((word >> lane) & 1ull) && number >= got && number < round) entry[number] = e + lane;
-                const int taken = total > skip ? total - skip : 0;
-                got = got + taken < round ? got + taken : round;
-                skip = skip > total ? skip - total : 0;
+    if (count > 0) {
+        Notes notes;
+        notes.read(p, b);
+        const Entries at = entries_of(p, b);
+        for (int done = 0; done < count; done += kRound) {
+            const int round = count - done < kRound ? count - done : kRound;
+            if (wave == 0) {
+                const int n = free_pages(p, notes, notes.before + done, round, pages);
+                if (lane == 0) found = n;
+            } else if (wave == 1) {      // the entries of this round, from where the last one ended
+                int got = 0, skip = done;
+                for (int e = at.lo & ~63; e < at.hi && got < round; e += 64) {
+                    const unsigned long long word = p.lacks[(size_t)b * p.words + (e >> 6)];
+                    const int total = __builtin_popcountll(word), number = __builtin_popcountll(word & ((1ull << lane) - 1ull)) - skip + got;
+                    if (((word >> lane) & 1ull) && number >= got && number < round) entry[number] = e + lane;
+                    const int taken = total > skip ? total - skip : 0;
+                    got = got + taken < round ? got + taken : round;
+                    skip = skip > total ? skip - total : 0;
+                }
             }
+            __syncthreads();
+            if (done == 0) target = found > 0 ? pages[0] : -1;
+            if ((int)threadIdx.x < round) {
+                int32_t *at_entry = const_cast<int32_t *>(p.batch.table) + (size_t)b * p.batch.table_width + entry[threadIdx.x];
+                const int old = *at_entry, page = (int)threadIdx.x < found ? pages[threadIdx.x] : -1;
+                if (is_page(old, p.pool.pages)) count_by(p.pool.refs + old, -1);
+                if (page >= 0) p.pool.refs[page] = 1;
+                *at_entry = page;
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        if (done == 0) target = found > 0 ? pages[0] : -1;
-        if (!writes) break;
-        if ((int)threadIdx.x < round) {
-            int32_t *at_entry = const_cast<int32_t *>(p.batch.table) + (size_t)b * p.batch.table_width + entry[threadIdx.x];
-            const int old = *at_entry, page = (int)threadIdx.x < found ? pages[threadIdx.x] : -1;
-            if (is_page(old, p.pool.pages)) count_by(p.pool.refs + old, -1);
-            if (page >= 0) p.pool.refs[page] = 1;
-            *at_entry = page;
+        if (p.copies && threadIdx.x < 3) {
+            const bool any = shared >= 0 && target >= 0;
+            p.copies[3 * b + threadIdx.x] = threadIdx.x == 0 ? any ? shared : -1 : threadIdx.x == 1 ? any ? target : -1 : any ? at.before - (at.lo << p.pool.page_shift) : 0;
         }
-        __syncthreads();
+        return;
     }
-    if (writes && p.copies && threadIdx.x < 3) {
-        const bool any = shared >= 0 && target >= 0;
-        p.copies[3 * b + threadIdx.x] = threadIdx.x == 0 ? any ? shared : -1 : threadIdx.x == 1 ? any ? target : -1 : any ? held : 0;
-    }
-    if (shared >= 0 && target >= 0 && p.cache.k) copy_page(p.cache, p.cache, target, shared, held, part, gridDim.y);
+    if (p.copies && threadIdx.x < 3) p.copies[3 * b + threadIdx.x] = threadIdx.x < 2 ? -1 : 0;
 }
 
 __global__ __launch_bounds__(256) void kv_copy_pages_kernel(KvCache to, KvCache from, const int32_t *copies) {
@@ -261,10 +265,10 @@ __global__ __launch_bounds__(256) void kv_copy_pages_kernel(KvCache to, KvCache 
 
 __global__ void kv_none_missing_kernel(int32_t *missing) { *missing = 0; }
 
-// Workgroups of a copy: until the chip is full, no more than give each 16 KB.
+// Workgroups of a copy: one for each 16 KB of a head's keys or values, but no more than fill the chip twice (256 CUs, eight each).
 int copy_parts(long long copies, const KvCache &c) {
-    const long long most = ((long long)c.heads * 2 * c.dim << c.page_shift) / 16384, room = 2048 / (copies < 1 ? 1 : copies), n = room < most ? room : most;
-    return n < 1 ? 1 : (int)n;
+    const long long chunks = (((long long)c.dim << c.page_shift) + 16383) / 16384, most = chunks * 2 * c.heads, room = 4096 / (copies < 1 ? 1 : copies), n = room < most ? room : most;
+    return n < 1 ? 1 : n > 65000 ? 65000 : (int)n;
 }
 
 }  // namespace
@@ -283,11 +287,11 @@ KvReservePlan plan_kv_reserve(int pages, int sequences, int width) {
 }
 
 hipError_t launch_kv_release(const KvPool &pool, int32_t *table, const int32_t *first, const int32_t *last, int sequences, int width, hipStream_t stream) {
-    kv_release_kernel<<<(uint32_t)(((long long)sequences * width + 255) / 256), 256, 0, stream>>>(pool, table, first, last, sequences, width);
+    kv_release_kernel<<<dim3((width + 255) / 256, sequences), 256, 0, stream>>>(pool, table, first, last, width);
     return hipGetLastError();
 }
 hipError_t launch_kv_fork(const KvForkParams &p, hipStream_t stream) {
-    kv_fork_kernel<<<(uint32_t)(((long long)p.sequences * p.to_width + 255) / 256), 256, 0, stream>>>(p);
+    kv_fork_kernel<<<dim3((p.to_width + 255) / 256, p.sequences), 256, 0, stream>>>(p);
     return hipGetLastError();
 }
 hipError_t launch_kv_reserve(const KvReserveParams &p, hipStream_t stream) {
@@ -298,7 +302,7 @@ hipError_t launch_kv_reserve(const KvReserveParams &p, hipStream_t stream) {
     kv_reserve_plan_kernel<<<p.slices + (p.batch.sequences + 3) / 4, 256, 0, stream>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    kv_reserve_kernel<<<dim3(p.batch.sequences, p.cache.k ? copy_parts(p.batch.sequences, p.cache) : 1), 256, 0, stream>>>(p);
+    kv_reserve_kernel<<<dim3(p.batch.sequences, p.cache.k ? 1 + copy_parts(p.batch.sequences, p.cache) : 1), 256, 0, stream>>>(p);
     return hipGetLastError();
 }
 hipError_t launch_kv_copy_pages(const KvCache &to, const KvCache &from, const int32_t *copies, int n, hipStream_t stream) {
