@@ -170,24 +170,11 @@ __device__ __forceinline__ float kv_squares(const float (&x)[8]) {      // two s
 
 // Eight channels at each of N places of one row of 16-bit queries at position `pos`, rotated, in fp32; place(i) is a multiple of 8.  In the order of halves
 // the partners of eight neighbours are eight neighbours, in the interleaved order they are among themselves (dims is a multiple of 16).  Everything
-// is requested before the first is used; channels past `dims` are loaded like the others and left as they are.  WEIGHTS: and normalised before, `ready` takes a run of
-// eight, and the weights for it.
-template <int N, bool WEIGHTS = false>
+// is requested before the first is used; channels past `dims` are loaded like the others and left as they are.
+template <int N>
 struct KvRotating {
     uint4 own[N], other[N];
     float c[N][8], s[N][8];
-    float w[WEIGHTS ? N : 1][8], w_other[WEIGHTS ? N : 1][8];
-    // of the row's weights, null: ones
-    template <typename Place>
-    __device__ __forceinline__ void request_weights(const float *weights, const KvRope &rope, Place place) {
-        const int half = rope.dims / 2;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int d = place(i) < rope.dims ? place(i) : 0;
-            kv_load_weights(weights, place(i), w[WEIGHTS ? i : 0]);
-            if (rope.dims != 0 && !rope.interleaved) kv_load_weights(weights, d >= half ? d - half : d + half, w_other[WEIGHTS ? i : 0]);
-        }
-    }
     template <typename Place>
     __device__ __forceinline__ void request(const uint16_t *row, const KvRope &rope, int pos, Place place) {
 #pragma unroll
@@ -211,15 +198,8 @@ struct KvRotating {
     }
     template <typename Place>
     __device__ __forceinline__ void finish(const KvRope &rope, Place place, float (&x)[N][8]) const {
-        finish(rope, place, x, [](float (&)[8], const float (&)[8]) {});
-    }
-    template <typename Place, typename Ready>
-    __device__ __forceinline__ void finish(const KvRope &rope, Place place, float (&x)[N][8], Ready ready) const {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            kv_floats(own[i], x[i]);
-            ready(x[i], w[WEIGHTS ? i : 0]);
-        }
+        for (int i = 0; i < N; ++i) kv_floats(own[i], x[i]);
         if (rope.dims == 0) return;
         if (rope.interleaved) {
 #pragma unroll
@@ -239,7 +219,6 @@ struct KvRotating {
         for (int i = 0; i < N; ++i) {
             float y[8];
             kv_floats(other[i], y);
-            ready(y, w_other[WEIGHTS ? i : 0]);
             const bool turn = place(i) < rope.dims, second = place(i) >= half;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {

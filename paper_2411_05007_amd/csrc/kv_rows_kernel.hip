@@ -19,6 +19,7 @@
 // heads, where the eight CUs draw 52 GB/s each.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "buffer.h"
 #include "kernels.h"
@@ -36,19 +37,99 @@ constexpr int WAVES = 4;
 template <int D>
 struct Block { uint4 k[2][D / 64]; uint4 v[D / 32]; };      // 32 tokens of a head, as a lane holds them
 
-// floats of a row in LDS, and the bytes of a workgroup's LDS: first the queries as operands in fp32 and maxima per wavefront, then [wave][row][row_floats] and maximum and sum
+// floats of a row in LDS, and the bytes of a workgroup's LDS: first the queries as operands in fp32 and maxima (and sums of squares) per wavefront, then [wave][row][row_floats] and maximum and sum
 // [wave][16][2], or, where parts meet, weights [chunk][row] and 16 bytes a thread
 constexpr int row_floats(int D) { return D + 4; }
-constexpr int rows_lds_bytes(int D, int waves, int cap, int chunks) {
-    const int loop = (waves * cap * row_floats(D) + waves * 32) * 4, queries = (D / 32 * 512 + waves * 64) * 4, parts = chunks > 1 ? (chunks * cap + 4) * 4 + waves * 64 * 16 : 0;
+constexpr int rows_lds_bytes(int D, int waves, int cap, int chunks, bool norm) {
+    const int loop = (waves * cap * row_floats(D) + waves * 32) * 4, queries = (D / 32 * 512 + waves * (norm ? 192 : 64)) * 4, parts = chunks > 1 ? (chunks * cap + 4) * 4 + waves * 64 * 16 : 0;
     return loop > parts ? loop > queries ? loop : queries : parts > queries ? parts : queries;
 }
 constexpr int kAgent = 16;      // cache policy of a buffer access that all XCDs see
 
-// MORE: with a norm of the queries, or with first tokens that stay visible before a window (else the launch has neither).  Blocks count on without a gap then: first those of the
-// first tokens, then the window's, from v0 on; block_of() says which block of the sequence that is.
-template <int D, bool MORE>
+// As KvRotating, of a row that is normalised first.  The factor r of the norm is the same for all channels of a row, so it waits: what is turned is x w 2^-32 (which no finite x takes past
+// fp32), and r 2^32 goes into the row's factor of the scores, when the wavefronts' sums of squares have met beside their maxima.
+// Every load is made whatever the call needs (from `any`, 32 D bytes that may be read, where there is nothing else), so that no branch lies between the block table's entry, which
+// is waited for next, and what was asked for behind it.
+constexpr float kHeld = 2.3283064365386963e-10f;      // 2^-32
+template <int N>
+struct KvReadying {
+    uint4 own[N], other[N];
+    float c[N][8], s[N][8], w[N][8], w_other[N][8];
+    bool ones;
+    template <typename Place>
+    __device__ __forceinline__ void request(const uint16_t *row, const KvNorm &norm, const KvRope &rope, int pos, int head, Place place, const uint8_t *any) {
+        const float *spare = reinterpret_cast<const float *>(any), *weights = kv_norm_row(norm, pos, head);
+        const float *t = rope.dims ? rope.table + (size_t)(pos < 0 ? 0 : pos < rope.positions ? pos : rope.positions - 1) * rope.dims : spare;
+        const int half = rope.dims / 2;
+        ones = weights == nullptr;
+        weights = ones ? spare : weights;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int d = place(i) < rope.dims ? place(i) : 0;
+            const int first = rope.interleaved ? d / 2 : d >= half ? d - half : d, more = rope.interleaved ? 0 : 4;      // (interleaved: the first four of each)
+            const int partner = d >= half ? d - half : d + half;
+            own[i] = *reinterpret_cast<const uint4 *>(row + place(i));
+            other[i] = *reinterpret_cast<const uint4 *>(row + partner);
+            kv_load8(weights + place(i), w[i]);
+            kv_load8(weights + partner, w_other[i]);
+            const kv_floatx4 a = *reinterpret_cast<const kv_floatx4 *>(t + first), b = *reinterpret_cast<const kv_floatx4 *>(t + first + more);
+            const kv_floatx4 e = *reinterpret_cast<const kv_floatx4 *>(t + half + first), f = *reinterpret_cast<const kv_floatx4 *>(t + half + first + more);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                c[i][k] = a[k]; c[i][4 + k] = b[k];
+                s[i][k] = e[k]; s[i][4 + k] = f[k];
+            }
+        }
+    }
+    // sum, tiny: of the squares of run i's numbers, and of 2^-72 times them
+    __device__ __forceinline__ void add_squares(int i, float &sum, float &tiny) const {
+        float y[8];
+        kv_floats(own[i], y);
+        sum += kv_squares(y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] *= kKvTiny;
+        tiny += kv_squares(y);
+    }
+    template <typename Place>
+    __device__ __forceinline__ void finish(const KvRope &rope, Place place, float (&x)[N][8]) const {
+        const auto ready = [&](const uint4 &raw, const float (&weight)[8], float (&y)[8]) {
+            kv_floats(raw, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= ones ? kHeld : weight[e] * kHeld;
+        };
+#pragma unroll
+        for (int i = 0; i < N; ++i) ready(own[i], w[i], x[i]);
+        if (rope.dims == 0) return;
+        const int half = rope.dims / 2;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool turn = place(i) < rope.dims, second = place(i) >= half;
+            if (rope.interleaved) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = x[i][2 * e], b = x[i][2 * e + 1];
+                    x[i][2 * e] = turn ? kv_turn_a(a, b, c[i][e], s[i][e]) : a;
+                    x[i][2 * e + 1] = turn ? kv_turn_b(a, b, c[i][e], s[i][e]) : b;
+                }
+            } else {
+                float y[8];
+                ready(other[i], w_other[i], y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float z = second ? kv_turn_b(y[e], x[i][e], c[i][e], s[i][e]) : kv_turn_a(x[i][e], y[e], c[i][e], s[i][e]);
+                    x[i][e] = turn ? z : x[i][e];
+                }
+            }
+        }
+    }
+};
+
+// Of a launch: kPlain has neither a norm of the queries nor first tokens that stay visible before a window, kSinks has those, kNorm a norm and those, if there are any.  With first
+// tokens blocks count on without a gap: first theirs, then the window's, from v0 on; block_of() says which block of the sequence that is.
+enum Kind { kPlain, kSinks, kNorm };
+template <int D, Kind KIND>
 __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_rows_kernel(KvAttentionParams p) {
+    constexpr bool SINKS = KIND != kPlain, NORM = KIND == kNorm;
     constexpr int C = D / 32;                    // runs of 32 channels = steps of K Q^T per 16 tokens
     constexpr int kRow = row_floats(D);
     extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -68,7 +149,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     const int seen_hi = hi_of(pos);
     const int seen_lo = p.causal && p.window > 0 && pos + 1 > p.window ? pos + 1 - p.window : 0;
     // keys of the row between the first tokens and its window
-    const int hidden = MORE && p.sinks < seen_lo ? p.sinks : seen_lo;
+    const int hidden = SINKS && p.sinks < seen_lo ? p.sinks : seen_lo;
     const uint32_t hidden_count = (uint32_t)(seen_lo - hidden);
     // of the tile: its first row sees the fewest and the earliest keys
     const int tok_a = tile * 16 / p.group, last = tile * 16 + 15 < rows ? tile * 16 + 15 : rows - 1, tok_z = last / p.group;
@@ -76,8 +157,8 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     const int any_hi = hi_of(pos_z), all_hi = hi_of(pos_a);
     const int any_lo = p.causal && p.window > 0 && pos_a + 1 > p.window ? pos_a + 1 - p.window : 0, all_lo = p.causal && p.window > 0 && pos_z + 1 > p.window ? pos_z + 1 - p.window : 0;
     const int blk0 = any_lo >> 5, blk1 = (any_hi + 31) >> 5;
-    const int sinks = MORE ? p.sinks : 0, sink_blocks = (int)(((long long)sinks + 31) >> 5), v0 = MORE ? blk0 - (sink_blocks < blk0 ? sink_blocks : blk0) : blk0;
-    const auto block_of = [&](int v) { return MORE && v < blk0 ? v - v0 : v; };
+    const int sinks = SINKS ? p.sinks : 0, sink_blocks = (int)(((long long)sinks + 31) >> 5), v0 = SINKS ? blk0 - (sink_blocks < blk0 ? sink_blocks : blk0) : blk0;
+    const auto block_of = [&](int v) { return SINKS && v < blk0 ? v - v0 : v; };
     // this workgroup's blocks
     const int chunk = blockIdx.x, count = blk1 > blk0 ? blk1 - v0 : 0;
     int nchunks = (count + p.chunk_blocks - 1) / p.chunk_blocks;
@@ -124,15 +205,10 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
         const int c = wave * kMine + i < C ? wave * kMine + i : C - 1;
         return 64 * (c / 2) + 16 * q4 + 8 * (c % 2);
     };
-    KvRotating<kMine, MORE> turning;
+    std::conditional_t<NORM, KvReadying<kMine>, KvRotating<kMine>> turning;
     const uint16_t *row = p.q.data + (size_t)(t0 + tok) * p.q.token_stride + qh * p.q.head_stride;
-    turning.request(row, p.rope, pos, place);
-    uint4 whole[MORE ? C : 1];      // the row's other channels too, for the mean of its squares
-    if (MORE && p.norm.on) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) whole[MORE ? c : 0] = *reinterpret_cast<const uint4 *>(row + 64 * (c / 2) + 16 * q4 + 8 * (c % 2));
-        turning.request_weights(kv_norm_row(p.norm, pos, qh), p.rope, place);
-    }
+    if constexpr (NORM) turning.request(row, p.norm, p.rope, pos, qh, place, p.cache.k);
+    else turning.request(row, p.rope, pos, place);
     __builtin_amdgcn_sched_barrier(0);
     look_up_bytes();
     Block<D> even, odd;
@@ -144,37 +220,9 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     float to_t;      // score -> exponent of 2, but for the block's scale
     {
         float x[kMine][8];
-        if (MORE && p.norm.on) {
-            const auto squares = [&](float by) {
-                float sum = 0.f;
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    float y[8];
-                    kv_floats(whole[MORE ? c : 0], y);
-                    if (by != 1.f) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) y[e] *= by;
-                    }
-                    sum += kv_squares(y);
-                }
-                return kv_sum32(kv_sum16(sum));
-            };
-            float sum = squares(1.f), by = 1.f, eps = p.norm.eps;
-            const bool large = !(sum < __builtin_inff());
-            if (__builtin_amdgcn_ballot_w64(large) != 0ull) {
-                by = large ? kKvTiny : 1.f;
-                eps = large ? 0.f : eps;
-                sum = squares(by);
-            }
-            const float factor = kv_norm_factor(sum, 1.f / D, eps);
-            turning.finish(p.rope, place, x, [&](float (&y)[8], const float (&w)[8]) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = y[e] * by * factor * w[e];
-            });
-        } else {
-            turning.finish(p.rope, place, x);
-        }
+        turning.finish(p.rope, place, x);
         uint32_t top = 0u;
+        float sum = 0.f, tiny = 0.f;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
 #pragma unroll
@@ -183,16 +231,32 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
                 top = top > u ? top : u;
             }
             if (wave * kMine + i < C) {
+                if constexpr (NORM) turning.add_squares(i, sum, tiny);
                 float *dst = lds + ((wave * kMine + i) * 64 + lane) * 8;
                 *reinterpret_cast<kv_floatx4 *>(dst) = kv_floatx4{x[i][0], x[i][1], x[i][2], x[i][3]};
                 *reinterpret_cast<kv_floatx4 *>(dst + 4) = kv_floatx4{x[i][4], x[i][5], x[i][6], x[i][7]};
             }
         }
         lds[C * 512 + wave * 64 + lane] = kv_max32(kv_max16(__uint_as_float(top >= 0x7f800000u ? 0x7f800000u : top)));
+        if (NORM) {
+            lds[C * 512 + (WAVES + wave) * 64 + lane] = kv_sum32(kv_sum16(sum));
+            lds[C * 512 + (2 * WAVES + wave) * 64 + lane] = kv_sum32(kv_sum16(tiny));
+        }
         kv_lds_barrier();
         float m = lds[C * 512 + lane];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) m = fmaxf(m, lds[C * 512 + w * 64 + lane]);
+        float factor = 1.f;
+        if (NORM) {
+            float squares[2] = {0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                squares[0] += lds[C * 512 + (WAVES + w) * 64 + lane];
+                squares[1] += lds[C * 512 + (2 * WAVES + w) * 64 + lane];
+            }
+            const bool large = !(squares[0] < __builtin_inff());
+            factor = kv_norm_factor(large ? squares[1] : squares[0], 1.f / D, large ? 0.f : p.norm.eps) * (large ? kKvTiny / kHeld : 1.f / kHeld);
+        }
         const int e = (int)(__float_as_uint(m) >> 23) - 127;                          // m in [2^e, 2^(e + 1))
         const int up = e < -100 ? 114 : e > 127 ? 0 : 14 - e;                         // (not finite: as it is, the row becomes NaN)
         const float f = kv_pow2(up);
@@ -205,7 +269,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
                 qf[c][4 + i] = (_Float16)(hi[i] * f);
             }
         }
-        to_t = p.scale * kv_pow2(-up);
+        to_t = p.scale * kv_pow2(-up) * factor;
     }
 
     kv_floatx4 o[D / 16] = {};
@@ -234,7 +298,7 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int key = first + (j & 3) + 8 * (j >> 2);
-                const bool ok = named && (MORE ? (uint32_t)(key - hidden) >= hidden_count : key >= seen_lo) && key < seen_hi && key < len;
+                const bool ok = named && (SINKS ? (uint32_t)(key - hidden) >= hidden_count : key >= seen_lo) && key < seen_hi && key < len;
                 t[j] = ok ? t[j] : -__builtin_inff();
                 if (!named || key >= len) live[j >> 2] &= ~(0xffu << (8 * (j & 3)));
             }
@@ -480,27 +544,31 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
     for (int i = threadIdx.x; i < nchunks; i += WAVES * 64) __hip_atomic_store(words + i, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <int D, bool MORE>
-hipError_t launch_rows(const KvAttentionParams &p, hipStream_t stream) {
+template <int D, Kind KIND>
+hipError_t launch_rows_of(const KvAttentionParams &p, hipStream_t stream) {
     static LdsLimit limit;
-    constexpr int most = rows_lds_bytes(D, WAVES, 16, kKvMostChunks);
+    constexpr int most = rows_lds_bytes(D, WAVES, 16, kKvMostChunks, KIND == kNorm);
     if (p.chunks > kKvMostChunks) return hipErrorInvalidValue;
     if (most > 65536) {
-        const hipError_t e = limit.raise(reinterpret_cast<const void *>(kv_rows_kernel<D, MORE>), most);
+        const hipError_t e = limit.raise(reinterpret_cast<const void *>(kv_rows_kernel<D, KIND>), most);
         if (e != hipSuccess) return e;
     }
-    kv_rows_kernel<D, MORE><<<dim3(p.chunks, p.cache.heads, p.batch.sequences * p.row_tiles), WAVES * 64, rows_lds_bytes(D, WAVES, p.row_cap, p.chunks), stream>>>(p);
+    kv_rows_kernel<D, KIND><<<dim3(p.chunks, p.cache.heads, p.batch.sequences * p.row_tiles), WAVES * 64, rows_lds_bytes(D, WAVES, p.row_cap, p.chunks, KIND == kNorm), stream>>>(p);
     return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_rows(const KvAttentionParams &p, hipStream_t stream) {
+    return p.norm.on ? launch_rows_of<D, kNorm>(p, stream) : p.sinks > 0 ? launch_rows_of<D, kSinks>(p, stream) : launch_rows_of<D, kPlain>(p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_kv_attention_rows(const KvAttentionParams &p, hipStream_t stream) {
-    const bool more = p.norm.on || p.sinks > 0;
     switch (p.cache.dim) {
-        case 64: return more ? launch_rows<64, true>(p, stream) : launch_rows<64, false>(p, stream);
-        case 128: return more ? launch_rows<128, true>(p, stream) : launch_rows<128, false>(p, stream);
-        case 256: return more ? launch_rows<256, true>(p, stream) : launch_rows<256, false>(p, stream);
+        case 64: return launch_rows<64>(p, stream);
+        case 128: return launch_rows<128>(p, stream);
+        case 256: return launch_rows<256>(p, stream);
         default: return hipErrorInvalidValue;
     }
 }
