@@ -290,8 +290,6 @@ struct KvAttentionParams {
     int q_heads, group;      // group = q_heads / cache.heads
     float scale;             // of the scores, times log2(e)
     int causal, window;      // window = 0: none
-    KvNorm norm;             // of the queries
-    int sinks;               // with a window: first tokens of a sequence that every row at or behind them sees
     int least_rows, most_rows;     // sequences with fewer rows a head are not for the many-row kernel, those with more not for the few-row kernel
     int tile_rows, parts;    // many-row kernel: rows of a workgroup (128 or 256), parts that the keys of a row tile are cut into
     int row_tiles;           // few-row kernel: tiles of 16 rows a sequence and head may need
@@ -300,6 +298,8 @@ struct KvAttentionParams {
     float *partial;          // chunks > 1: fp32 [sequence][row tile][head][chunk]([row_cap][dim] weighted means of values, [row_cap][2] maximum and sum of weights)
     float *part_ml;          // parts > 1: fp32 [part][row][2] maximum and sum of weights, rows as in out; partial [part][row][dim]
     unsigned long long *arrived;      // chunks > 1: [sequence][row tile][head][chunk]
+    KvNorm norm;             // of the queries
+    int sinks;               // with a window: first tokens of a sequence that every row at or behind them sees
 };
 hipError_t launch_kv_attention_rows(const KvAttentionParams &p, hipStream_t stream);      // few rows (kv_rows_kernel.hip)
 hipError_t launch_kv_attention_tile(const KvAttentionParams &p, hipStream_t stream);      // many (kv_tile_kernel.hip)

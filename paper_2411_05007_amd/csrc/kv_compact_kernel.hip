@@ -296,7 +296,8 @@ struct ValueMoves {
         if (whole) return;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bool moves = live(at.w, token(j)) && __shfl((int)src.unit, token(j)) != -1;
+            const int unit = __shfl((int)src.unit, token(j));      // (from all lanes: before any of them is left out)
+            const bool moves = live(at.w, token(j)) && unit != -1;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 x[i][0][j] = moves ? x[i][0][j] : 0.f;
