@@ -493,7 +493,8 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
  * count goes down.  Of a page that held tokens before the new ones, those are copied, in whole blocks of 32, in `cache` if it is given; copies (NULL, or device int32 [sequences][3])
  * says for each sequence (page, to page, tokens), (-1, -1, 0) if nothing is to be copied: with svdq_kv_copy_pages the caches of further layers follow.  missing (NULL, or device int32)
  * becomes the number of entries for which no page was left: they name none (the tokens there are neither written nor seen, and those that a shared page held are lost to the
- * sequence), nobody else's pages are touched.  workspace: device, 256-byte aligned, >= svdq_kv_pages_reserve_workspace_bytes(), no initial contents.  Two kernels; with the tables
+ * sequence), nobody else's pages are touched.  workspace: device, 256-byte aligned, >= svdq_kv_pages_reserve_workspace_bytes(), no initial contents; calls that
+ * share one are ordered on one stream.  Two kernels; with the tables
  * and counts of a captured graph's buffers it can be captured with the step.
  *
  * Copy: tokens c[i][2] (in whole blocks) of page c[i][0] of `from` to page c[i][1] of `to`; nothing where either names no page.  The caches are the same one or alike; no page is
@@ -519,8 +520,8 @@ int svdq_kv_copy_pages(const svdq_kv_cache_dev *to, const svdq_kv_cache_dev *fro
  * With a rope, keys are turned from the position that the token had to the one that it gets (the table that they were appended with; its rows need not have size one); a token
  * that keeps its position keeps its key.  Blocks are quantized as by an append of the moved vectors in that order: tokens before to_first[b] in its block stay, at the larger
  * byte; what lies behind the last move in its block is lost.  A token that no page of from_table holds becomes one with NaN codes, as do those that have some.
- *   workspace NULL: no page that is written is one that is read.  Otherwise (256-byte aligned, >= svdq_kv_compact_workspace_bytes(), no initial contents) pages may be read and
- *   written in the same call, as where a sequence shrinks in place; no page is written for two sequences.
+ *   workspace NULL: no page that is written is one that is read.  Otherwise (device, 256-byte aligned, >= svdq_kv_compact_workspace_bytes(), no initial contents; calls that share
+ *   one are ordered on one stream) pages may be read and written in the same call, as where a sequence shrinks in place; no page is written for two sequences.
  * One kernel, a second one with a workspace.  SVDQ_EINVAL and SVDQ_EUNSUPPORTED as above, SVDQ_EINVAL also for caches that do not fit each other.
  */
 typedef struct {

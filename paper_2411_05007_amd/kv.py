@@ -58,13 +58,16 @@ class KVNorm:
         given = [t for t in (q, k, q_first, k_first) if t is not None]
         for t in given:
             assert t.dtype is torch.float32 and t.is_cuda and t.is_contiguous() and t.dim() in (1, 2), "weights: contiguous fp32 [head_dim] or [heads, head_dim] on the GPU"
-        assert len({t.dim() for t in given}) <= 1, "weights: all for each head, or none"
+        assert len({(t.dim(), t.shape[-1]) for t in given}) <= 1, "weights: all for each head, or none, and of one head size"
+        for a, b in ((q, q_first), (k, k_first)):
+            assert a is None or b is None or a.shape == b.shape, "weights: of the first tokens as of the others"
+        heads = lambda a, b: next((t.shape[0] for t in (a, b) if t is not None and t.dim() == 2), None)
+        self.q_heads, self.k_heads, self.dim = heads(q, q_first), heads(k, k_first), given[0].shape[-1] if given else None      # (None: any)
         at = lambda t: None if t is None else t.data_ptr()
         self.cdesc = S.KVNormDev(at(q), at(k), at(q_first), at(k_first), int(first_tokens), int(bool(given) and given[0].dim() == 2), self.eps)
 
-    def _check(self, name: str, heads: int, dim: int) -> None:
-        for t in (getattr(self, name), getattr(self, name + "_first")):
-            assert t is None or tuple(t.shape) == ((heads, dim) if t.dim() == 2 else (dim,)), f"norm: weights of {tuple(t.shape)} for {heads} heads of {dim}"
+    def _check(self, held: Optional[int], heads: int, dim: int) -> None:
+        assert (self.dim is None or self.dim == dim) and (held is None or held == heads), f"norm: weights of {self.dim} channels and {held} heads for {heads} heads of {dim}"
 
 
 class KVBatch:
@@ -166,7 +169,7 @@ class KVCache:
         """k, v: bf16 [new_tokens, kv_heads, head_dim] (any token and head stride that keeps 16-byte alignment)."""
         kd, vd = self._rows(k, self.kv_heads, batch.new_tokens, "k"), self._rows(v, self.kv_heads, batch.new_tokens, "v")
         if norm is not None:
-            norm._check("k", self.kv_heads, self.head_dim)
+            norm._check(norm.k_heads, self.kv_heads, self.head_dim)
         S._check(S.lib().svdq_kv_append_normed(self.cdesc, batch.cdesc, None if norm is None else norm.cdesc, None if rope is None else rope.cdesc, kd, vd,
                                                self._stream(stream)), "svdq_kv_append")
 
@@ -191,7 +194,7 @@ class KVCache:
         else:
             assert workspace.dtype is torch.uint8 and workspace.is_cuda and workspace.is_contiguous(), "workspace: uint8 on the GPU"
         if norm is not None:
-            norm._check("q", heads, self.head_dim)
+            norm._check(norm.q_heads, heads, self.head_dim)
         S._check(S.lib().svdq_kv_attention_normed(self.cdesc, batch.cdesc, None if norm is None else norm.cdesc, None if rope is None else rope.cdesc, qd, heads,
                                                   1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(causal), int(window), int(sinks), out.data_ptr(),
                                                   workspace.data_ptr(), workspace.numel(), self._stream(stream)), "svdq_kv_attention")

@@ -244,7 +244,8 @@ def test_weights_of_the_wrong_shape_are_refused(torch, KV):
             w.cache.append(x[:, 4:6], x[:, 6:], batch, norm=norm)
         with pytest.raises(AssertionError):
             w.cache.attention(x[:, :4], batch, norm=norm)
-    for make in (lambda: KV.KVNorm(t(64), t(2, 64)), lambda: KV.KVNorm(t(64).half()), lambda: KV.KVNorm(t(128)[::2])):
+    for make in (lambda: KV.KVNorm(t(64), t(2, 64)), lambda: KV.KVNorm(t(64).half()), lambda: KV.KVNorm(t(128)[::2]), lambda: KV.KVNorm(t(4, 64), q_first=t(2, 64)),
+                 lambda: KV.KVNorm(t(64), t(128)), lambda: KV.KVNorm(t(1, 2, 64))):
         with pytest.raises(AssertionError):
             make()
 
