@@ -14,9 +14,10 @@
 // wavefront, three workgroups a CU), each requested right behind the last use of its registers.
 // The wavefronts meet in LDS, as weighted means.  With several chunks the parts lie in the workspace, past the L2s, and the workgroup that finds all of its row tile
 // arrived joins them in chunk order (the same bits whoever it is), eight requests in flight a thread; nothing waits for another workgroup.
+// First tokens that stay visible before a window are blocks before the window's: the chunks count on over the gap, which is not read.
 // Bound: memory, one byte per channel of a key and a value: one sequence of 131071 keys, 8 key heads of 128, 32 query heads 54 us (5.0 TB/s), 64 sequences
-// of 100 to 16384 keys 245 us (4.65 TB/s).  Short ones by a chain of round trips: 5.7 us for one block (lengths, table, codes, queries turned on the way), 9.3 us for 777 keys of eight
-// heads, where the eight CUs draw 52 GB/s each.
+// of 100 to 16384 keys 245 us (4.65 TB/s); of 100 to 32768 in a window of 8192 with 64 first tokens and normalised queries 195 us (4.83 TB/s, 193 without either).  Short ones by a chain of round trips: 5.7 us for one block (lengths, table, codes, queries turned on the way), 9.3 us for 777 keys of eight
+// heads, where the eight CUs draw 52 GB/s each; 11.4 for 1024 keys and four first tokens, normalised queries, in five pieces (10.9 without).  Eight wavefronts a workgroup gain nothing: 13.0.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <type_traits>

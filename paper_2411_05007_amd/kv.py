@@ -1,10 +1,19 @@
-"""Binding of the paged 8-bit cache of keys and values and of the attention over it (``svdq_kv_*`` in ``include/svdq.h``).
+"""Binding of the paged 8-bit cache of keys and values, of the attention over it and of its pages (``svdq_kv_*`` in ``include/svdq.h``).
 
     cache = KVCache(pages, kv_heads, head_dim, page_tokens)
     batch = KVBatch(cu_new, kv_len, block_table, new_tokens, max_new, max_len)
     q, k, v = split_heads(qkv, q_heads, kv_heads)                     # views of a QKV layer's output
     cache.append(k, v, batch, rope)                                   # keys rotated, both quantized
     out = cache.attention(q, batch, rope)                             # bf16 [tokens, q_heads, head_dim]
+
+A stream that outlives its window, in pages that are handed out and given back on the GPU:
+
+    norm, pool = KVNorm(q_weight, k_weight), KVPages(pages, page_tokens)
+    pool.reserve(cache, batch)                                        # the new tokens' pages
+    cache.append(k, v, batch, rope, norm=norm)
+    out = cache.attention(q, batch, rope, window=4096, sinks=4, norm=norm)
+    pool.release(batch.block_table, first_token, end_token)           # what lies between the first tokens and the window
+    cache.compact(moves, rope)                                        # or: some tokens become a sequence's only ones
 
 Argument marshalling only; every call enqueues on the current stream (or the one that is given) and does not synchronise.  A stream that is given is the caller's to order
 behind what makes the inputs, and before what reads the results.
