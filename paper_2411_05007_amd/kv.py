@@ -271,30 +271,29 @@ class KVPages:
     _stream, _new = KVCache._stream, KVCache._new
 
     @staticmethod
-    def _table(t, name: str) -> None:
-        _device_int32(t, name)
-        assert t.dim() == 2, f"{name}: [sequences, width]"
+    def _table(t, name: str):
+        assert t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.dim() == 2, f"{name}: contiguous int32 [sequences, width] on the GPU"
+        return t.shape
+
+    @staticmethod
+    def _one_each(t, rows: int, name: str) -> int:
+        assert t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.dim() == 1 and t.numel() == rows, f"{name}: contiguous int32 on the GPU, one for each row"
+        return t.data_ptr()
 
     def release(self, block_table, first_token=None, end_token=None, stream=None) -> None:
         """Gives back the pages wholly within tokens first_token[b] .. end_token[b] - 1 of each row (None: from 0, to the end); the entries become -1."""
-        self._table(block_table, "block_table")
-        at = [None, None]
-        for i, t in enumerate((first_token, end_token)):
-            if t is not None:
-                _device_int32(t, ("first_token", "end_token")[i])
-                assert t.shape == (block_table.shape[0],)
-                at[i] = t.data_ptr()
-        S._check(S.lib().svdq_kv_pages_release(self.cdesc, block_table.data_ptr(), *at, *block_table.shape, self._stream(stream)), "svdq_kv_pages_release")
+        rows, width = self._table(block_table, "block_table")
+        first = None if first_token is None else self._one_each(first_token, rows, "first_token")
+        end = None if end_token is None else self._one_each(end_token, rows, "end_token")
+        S._check(S.lib().svdq_kv_pages_release(self.cdesc, block_table.data_ptr(), first, end, rows, width, self._stream(stream)), "svdq_kv_pages_release")
 
     def fork(self, from_table, from_len, parent, to_table, to_len, stream=None) -> None:
         """Rows of to_table take the pages of rows parent[i] of from_table, to_len[i] becomes from_len[parent[i]].  What to_table named before is to be released first."""
-        self._table(from_table, "from_table")
-        self._table(to_table, "to_table")
-        for t, n, rows in ((from_len, "from_len", from_table), (parent, "parent", to_table), (to_len, "to_len", to_table)):
-            _device_int32(t, n)
-            assert t.shape == (rows.shape[0],), f"{n}: one for each row"
-        S._check(S.lib().svdq_kv_pages_fork(self.cdesc, from_table.data_ptr(), from_len.data_ptr(), *from_table.shape, parent.data_ptr(), to_table.data_ptr(), to_len.data_ptr(),
-                                            *to_table.shape, self._stream(stream)), "svdq_kv_pages_fork")
+        parents, from_width = self._table(from_table, "from_table")
+        rows, to_width = self._table(to_table, "to_table")
+        S._check(S.lib().svdq_kv_pages_fork(self.cdesc, from_table.data_ptr(), self._one_each(from_len, parents, "from_len"), parents, from_width,
+                                            self._one_each(parent, rows, "parent"), to_table.data_ptr(), self._one_each(to_len, rows, "to_len"), rows, to_width,
+                                            self._stream(stream)), "svdq_kv_pages_fork")
 
     def reserve_workspace(self, batch: KVBatch, stream=None):
         """For reserve(): its notes, and what further caches copy."""
