@@ -486,7 +486,7 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
  *
  * Fork: row i of to_table becomes the pages that hold the tokens of row parent[i] of from_table, -1 behind them, and to_len[i] their number from_len[parent[i]] (up to what either
  * table holds; nothing for a parent outside 0 .. from_sequences - 1); counts go up.  Several rows may have one parent.  What the rows of to_table named before is not given
- * back: release it first.  The two tables, and the two arrays of lengths, do not overlap (SVDQ_EINVAL).
+ * back: release it first.  The two tables, and the two arrays of lengths, do not overlap, nor does parent with what is written (SVDQ_EINVAL).
  *
  * Reserve: makes every page that the batch's new tokens fall in exist and be the sequence's own; call it before svdq_kv_append.  Among the entries of positions kv_len - n ..
  * kv_len - 1, those that name no page, or one whose count is above one, get the lowest pages that were free at the call, in the order of sequences and entries; the old page's

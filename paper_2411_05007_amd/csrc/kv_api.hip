@@ -209,7 +209,9 @@ int svdq_kv_pages_fork(const svdq_kv_pool_dev *pool, const int32_t *from_table, 
     if (!parent || !to_len || (from_sequences > 0 && !from_len) || (((uintptr_t)from_len | (uintptr_t)parent | (uintptr_t)to_len) & 3)) return SVDQ_EINVAL;
     // (rows are read while others are written)
     const size_t from_bytes = (size_t)from_sequences * from_width * 4, to_bytes = (size_t)sequences * to_width * 4;
-    if (overlap(from_table, from_bytes, to_table, to_bytes) || overlap(from_len, (size_t)from_sequences * 4, to_len, (size_t)sequences * 4)) return SVDQ_EINVAL;
+    const size_t each = (size_t)sequences * 4;
+    if (overlap(from_table, from_bytes, to_table, to_bytes) || overlap(from_len, (size_t)from_sequences * 4, to_len, each)) return SVDQ_EINVAL;
+    if (overlap(parent, each, to_len, each) || overlap(parent, each, to_table, to_bytes)) return SVDQ_EINVAL;
     const svdq::KvForkParams p{pool_of(pool), from_table, from_len, parent, to_table, to_len, from_sequences, from_width, sequences, to_width};
     return done(svdq::launch_kv_fork(p, static_cast<hipStream_t>(hip_stream)));
 }

@@ -124,6 +124,12 @@ def test_tables_that_are_refused(lib):
     assert fork(m=0) == 0
 
 
+def test_parents_that_are_written_are_refused(lib):
+    fork = lambda parent, t=FAR, tl=FAR + 4096, m=4, tw=6: lib.svdq_kv_pages_fork(pool(), AT, AT, 3, 5, parent, t, tl, m, tw, None)
+    assert fork(FAR + 4096) == fork(FAR + 4096 + 12) == fork(FAR + 4096 - 12) == EINVAL      # parent and to_len: each workgroup reads the one, the first writes the other
+    assert fork(FAR) == fork(FAR + 92) == fork(FAR - 12) == EINVAL                           # parent and to_table
+
+
 def test_reservations_that_are_refused(lib):
     p = pool()
     need = lib.svdq_kv_pages_reserve_workspace_bytes(p, 3, 2)
