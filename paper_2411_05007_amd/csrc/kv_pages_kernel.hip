@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256) void kv_reserve_plan_kernel(KvReserveParams p)
 
 // Copies the blocks of a page's first tokens, part `part` of `parts` of it (a workgroup of 256): the keys and values of a head lie in a row, and go in chunks of 16 KB.
 __device__ __forceinline__ void copy_page(const KvCache &to, const KvCache &from, int to_page, int from_page, int tokens, int part, int parts) {
-    const int bs = to.page_shift - 5, most = 1 << bs, blocks = (tokens + 31) >> 5 < most ? (tokens + 31) >> 5 : most;
+    const int bs = to.page_shift - 5, most = 32 << bs, blocks = ((tokens < most ? tokens : most) + 31) >> 5;
     if (blocks <= 0) return;
     constexpr int kAhead = 4, kChunk = 256 * kAhead;
     const int pieces = blocks * 2 * to.dim, chunks = (pieces + kChunk - 1) / kChunk, items = to.heads * 2 * chunks;      // pieces of 16 bytes of a head's keys, or values
