@@ -309,6 +309,8 @@ class KVPages:
         """Pages of its own for every new token of the batch, whose block_table is written; tokens before them in a shared page are copied, in `cache` or, where layers
         have caches of their own, in each of a list of them.  missing: int32 [1] on the GPU, entries for which no page was left (they name none)."""
         caches = [cache] if isinstance(cache, KVCache) else list(cache)
+        for c in caches:
+            assert c.pages >= self.pages and c.page_tokens == self.page_tokens, f"cache: {c.pages} pages of {c.page_tokens} for a pool of {self.pages} of {self.page_tokens}"
         if missing is not None:
             _device_int32(missing, "missing")
             assert missing.numel() == 1

@@ -221,6 +221,17 @@ def test_pages_are_copied_between_caches(torch, KV, dim, heads, P):
     a.check()
 
 
+@pytest.mark.parametrize("pages,P", [(9, 64), (10, 32), (10, 128)])
+def test_caches_that_do_not_fit_the_pool_are_refused_before_anything_is_changed(torch, KV, pages, P):
+    w = Pool(torch, KV, 10, 64)
+    dev, host = empty(torch, 1, 4)
+    other = KV.KVCache(pages, 2, 64, P)
+    for caches in ([w.caches[0], other], [other, w.caches[0]], other):      # (a further layer's as well as the first one's)
+        with pytest.raises(AssertionError):
+            w.pool.reserve(caches, KV.KVBatch(i32(torch, [0, 70]), i32(torch, [70]), dev, 70, 70, 70))
+    w.check((dev, host))
+
+
 def test_branches_in_a_captured_step(torch, KV):
     """Release, fork, reserve and append in one graph, replayed with other parents and with eager work between: every replay as the eager calls."""
     B, P, H, D = 6, 64, 2, 64
