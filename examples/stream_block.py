@@ -32,12 +32,13 @@ class StreamBlock(AttentionBlock):
 
     def buffers(self, batch, cache):
         B, i32 = batch.sequences, dict(dtype=torch.int32, device=DEV)
-        return {**super().buffers(batch, cache), "pages_ws": self.pool.reserve_workspace(batch), "missing": torch.zeros(1, **i32),
+        return {**super().buffers(batch, cache), "pages_ws": self.pool.reserve_workspace(batch), "missing": torch.zeros(1, **i32), "lost": torch.zeros(1, **i32),
                 "first": torch.full((B,), (SINKS + PAGE - 1) // PAGE * PAGE, **i32), "end": torch.zeros(B, **i32)}
 
     def __call__(self, x, cache, batch, buf):
         q, k, v = KV.split_heads(self.qkv.forward(x, buf["qkv"], buf["qkv_ws"]), Q_HEADS, KV_HEADS)
         self.pool.reserve(cache, batch, buf["missing"], workspace=buf["pages_ws"])
+        buf["lost"].add_(buf["missing"])      # of all steps: each writes `missing` anew
         cache.append(k, v, batch, self.rope, norm=self.norm)
         a = cache.attention(q, batch, self.rope, window=WINDOW, sinks=SINKS, norm=self.norm, out=buf["attention"], workspace=buf["attention_ws"])
         torch.sub(batch.kv_len, WINDOW - 1, out=buf["end"])      # the next token's window begins there
@@ -61,7 +62,7 @@ def main(tokens: int = 600, fmt: str = "int4", verbose: bool = True):
     batch = KV.KVBatch(i32([0, prompts[0], sum(prompts)]), i32(prompts), parents, sum(prompts), max(prompts), max(prompts))
     buf = block.buffers(batch, cache)
     block(torch.randn(sum(prompts), HIDDEN, generator=gen, device=DEV).to(torch.bfloat16), cache, batch, buf)
-    assert buf["missing"].item() == 0
+    assert buf["lost"].item() == 0
 
     table, length = none(B), i32([0] * B)
     pool.fork(parents, i32(prompts), i32([b // branches for b in range(B)]), table, length)
@@ -85,7 +86,7 @@ def main(tokens: int = 600, fmt: str = "int4", verbose: bool = True):
         graph.replay()
     end.record()
     torch.cuda.synchronize()
-    assert buf["missing"].item() == 0 and length.tolist() == [n + tokens for n in prompts for _ in range(branches)]
+    assert buf["lost"].item() == 0 and length.tolist() == [n + tokens for n in prompts for _ in range(branches)]
 
     error, rope = 0.0, block.rope.table.double()
     for b in range(B):

@@ -493,7 +493,10 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
  * count goes down.  Of a page that held tokens before the new ones, those are copied, in whole blocks of 32, in `cache` if it is given; copies (NULL, or device int32 [sequences][3])
  * says for each sequence (page, to page, tokens), (-1, -1, 0) if nothing is to be copied: with svdq_kv_copy_pages the caches of further layers follow.  missing (NULL, or device int32)
  * becomes the number of entries for which no page was left: they name none (the tokens there are neither written nor seen, and those that a shared page held are lost to the
- * sequence), nobody else's pages are touched.  workspace: device, 256-byte aligned, >= svdq_kv_pages_reserve_workspace_bytes(), no initial contents; calls that
+ * sequence), nobody else's pages are touched.  A sequence's first entry that names no page while tokens before the new ones fall in it gets none either, is counted in missing and stays as it
+ * is: those tokens are nowhere, and a page that was another sequence's would show its tokens in their place.  So after a shortage a sequence goes on without the rest of that page, in every
+ * step till its tokens leave it; a call that is repeated with the same lengths, once there is room, gets what it lacked but for the first entry that had tokens before.  What a captured step
+ * misses is added up on the GPU (missing is written anew by each call).  workspace: device, 256-byte aligned, >= svdq_kv_pages_reserve_workspace_bytes(), no initial contents; calls that
  * share one are ordered on one stream.  Two kernels; with the tables
  * and counts of a captured graph's buffers it can be captured with the step.
  *

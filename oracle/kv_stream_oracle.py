@@ -144,7 +144,8 @@ class Pages:
                     self.refs[g] += 1
 
     def reserve(self, table, new, lens):
-        """The copies (page, to page, tokens) of every sequence, and how many entries got no page."""
+        """The copies (page, to page, tokens) of every sequence, and how many entries got no page.  An entry that names no page, of a page whose first tokens are no new ones, gets
+        none: nothing holds those tokens, and a page that was another's would show its."""
         free = [g for g, n in enumerate(self.refs) if n <= 0]
         was, missing, copies = list(self.refs), 0, []
         for row, n, length in zip(table, new, lens):
@@ -154,6 +155,9 @@ class Pages:
             for e in range(before // self.P, (length + self.P - 1) // self.P) if n > 0 else ():
                 g = row[e]
                 if self.page(g) and was[g] <= 1:
+                    continue
+                if not self.page(g) and e * self.P < before:
+                    missing += 1
                     continue
                 if self.page(g):
                     self.refs[g] -= 1

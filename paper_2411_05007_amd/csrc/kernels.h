@@ -268,7 +268,7 @@ struct KvReserveParams {
     int32_t *copies;         // [sequences][3] or null: page, to page, tokens
     int32_t *missing;        // or null
     unsigned long long *free_words, *lacks;      // a bit a page; [sequences][words], a bit an entry
-    int32_t *slice_free, *lack_count, *shared;   // free pages of 1024; of a sequence the entries that lack a page, the page that it shares
+    int32_t *slice_free, *lack_count, *shared;   // free pages of 1024; of a sequence the entries that lack a page, the page that it shares (below zero: none, or none is to be given)
     int slices, words;
 };
 hipError_t launch_kv_release(const KvPool &pool, int32_t *table, const int32_t *first, const int32_t *last, int sequences, int width, hipStream_t stream);

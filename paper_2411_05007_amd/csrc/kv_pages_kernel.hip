@@ -4,7 +4,8 @@
 //   fork      a row of a table becomes the pages of another row's tokens; their counts go up
 //   release   entries of pages wholly within a range of tokens are cleared; their counts go down
 //   reserve   every entry that a batch's new tokens fall in names a page of the sequence's own: entries that name none, or one with a count above one, get the lowest free pages, in the
-//             order of sequences and entries, and what a shared page held before the new tokens is copied
+//             order of sequences and entries, and what a shared page held before the new tokens is copied.  A sequence's first entry that names none while tokens before the new ones fall in
+//             it (they found no page, or it was given back) gets none: nothing could fill those tokens' places, and another sequence's would be seen there
 //   copy      pages of one cache into pages of the same or another one
 // Reserve is two kernels.  The first notes what is free (a bit a page, counts for each 1024) and which entries lack a page (a bit an entry, a count for each sequence), the second
 // sums what comes before its sequence, enumerates the free pages from there and the entries side by side through LDS, and writes table and counts; further workgroups of the
@@ -53,6 +54,7 @@ __global__ __launch_bounds__(256) void kv_fork_kernel(KvForkParams p) {
 
 // ---- reserve ----------------------------------------------------------------------------------------------------------------
 constexpr int kSlicePages = 1024;      // pages of a count
+constexpr int kLost = -2;              // in the place of a shared page: the first entry is to stay without one
 struct Entries { int lo, hi, before; };      // of a sequence's table that its new tokens fall in; tokens before them
 __device__ __forceinline__ Entries entries_of(const KvReserveParams &p, int b) {
     const int cu0 = p.batch.cu[b], cu1 = p.batch.cu[b + 1], kv_len = p.batch.kv_len[b];
@@ -92,6 +94,7 @@ __global__ __launch_bounds__(256) void kv_reserve_plan_kernel(KvReserveParams p)
     const int b = ((int)blockIdx.x - p.slices) * 4 + wave;      // entries that lack a page
     if (b >= p.batch.sequences) return;
     const Entries at = entries_of(p, b);
+    const bool holds = (long long)at.lo << p.pool.page_shift < at.before;      // tokens before the new ones fall in the first entry
     int count = 0, shared = -1;
     for (int e0 = at.lo & ~63; e0 < at.hi; e0 += 64) {
         const int e = e0 + lane;
@@ -99,12 +102,15 @@ __global__ __launch_bounds__(256) void kv_reserve_plan_kernel(KvReserveParams p)
         const int page = lacks ? p.batch.table[(size_t)b * p.batch.table_width + e] : -1;
         const bool named = is_page(page, p.pool.pages);
         if (named) lacks = p.pool.refs[page] > 1;
+        const bool lost = lacks && !named && holds && e == at.lo;
+        lacks = lacks && !lost;
+        if (__builtin_amdgcn_ballot_w64(lost) != 0ull) shared = kLost;
         const unsigned long long word = __builtin_amdgcn_ballot_w64(lacks);
         if (lane == 0) p.lacks[(size_t)b * p.words + (e0 >> 6)] = word;
         count += __builtin_popcountll(word);
         if (e0 <= at.lo && at.lo < e0 + 64) {      // (what the first entry holds before the new tokens)
             const int first = __builtin_amdgcn_readlane(lacks && named ? page : -1, at.lo - e0);
-            if ((long long)at.lo << p.pool.page_shift < at.before) shared = first;
+            if (holds && shared != kLost) shared = first;
         }
     }
     if (lane == 0) {
@@ -209,12 +215,16 @@ __global__ __launch_bounds__(256) void kv_reserve_kernel(KvReserveParams p) {
         copy_page(p.cache, p.cache, target, shared, at.before - (at.lo << p.pool.page_shift), part - 1, (int)gridDim.y - 1);
         return;
     }
-    if (b == 0 && wave == 3 && p.missing) {      // entries that lack a page, in all, and free pages
-        int lack = 0;
-        for (int i = lane; i < p.batch.sequences; i += 64) lack += p.lack_count[i];
+    if (b == 0 && wave == 3 && p.missing) {      // entries that lack a page, in all, and free pages; entries that get none
+        int lack = 0, lost = 0;
+        for (int i = lane; i < p.batch.sequences; i += 64) {
+            lack += p.lack_count[i];
+            lost += p.shared[i] == kLost ? 1 : 0;
+        }
         for (int i = lane; i < p.slices; i += 64) lack -= p.slice_free[i];
         lack = wave_sum(lack);
-        if (lane == 0) *p.missing = lack > 0 ? lack : 0;
+        lost = wave_sum(lost);
+        if (lane == 0) *p.missing = (lack > 0 ? lack : 0) + lost;
     }
     int target = -1;      // of the copy: the first page
     if (count > 0) {
