@@ -138,8 +138,11 @@ __device__ __forceinline__ float kv_turn_fma_a(float a, float b, float c, float 
 __device__ __forceinline__ float kv_turn_fma_b(float a, float b, float c, float s) { return __builtin_fmaf(b, c, a * s); }
 
 // ---- norm of a head: y = x r w with r = 1 / sqrt(mean x^2 + eps), before the rotation ---------------------------------------------
-// Squares of numbers past 2^60 may leave fp32: rows whose sum does are taken 2^-72 times (eps is nothing beside them) and summed again, which happens in no ordinary call.
+// Squares of numbers past 2^60 may leave fp32: rows whose mean with eps does are taken 2^-72 times, eps 2^-144 times (it may be as large as they are), and summed again, which happens in
+// no ordinary call.
 constexpr float kKvTiny = 2.1175823681357508e-22f;      // 2^-72
+__device__ __forceinline__ bool kv_norm_leaves(float sum, float inv_dim, float eps) { return !(sum * inv_dim + eps < __builtin_inff()); }
+__device__ __forceinline__ float kv_norm_eps(bool large, float eps) { return large ? eps * kKvTiny * kKvTiny : eps; }
 __device__ __forceinline__ float kv_norm_factor(float sum, float inv_dim, float eps) {      // within half an ulp and little: a step of Newton's on the instruction's
     const float m = sum * inv_dim + eps, r = __builtin_amdgcn_rsqf(m);
     const float e = __builtin_fmaf(-(m * r), r, 1.f);
@@ -277,14 +280,14 @@ template <int U>
 __device__ __forceinline__ void kv_normalise(float (&x)[2][8], const float (&w)[2][8], float eps) {
     constexpr float kInverse = 1.f / (16 * U);
     float sum = kv_sum_lanes<U>(kv_squares(x[0]) + kv_squares(x[1]));
-    const bool large = !(sum < __builtin_inff());
+    const bool large = kv_norm_leaves(sum, kInverse, eps);
     if (__builtin_amdgcn_ballot_w64(large) != 0ull) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[j][e] = large ? x[j][e] * kKvTiny : x[j][e];
         sum = kv_sum_lanes<U>(kv_squares(x[0]) + kv_squares(x[1]));
-        eps = large ? 0.f : eps;
+        eps = kv_norm_eps(large, eps);
     }
     const float r = kv_norm_factor(sum, kInverse, eps);
 #pragma unroll

@@ -255,8 +255,8 @@ __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D > 64 ? 3 : 4) void kv_r
                 squares[0] += lds[C * 512 + (WAVES + w) * 64 + lane];
                 squares[1] += lds[C * 512 + (2 * WAVES + w) * 64 + lane];
             }
-            const bool large = !(squares[0] < __builtin_inff());
-            factor = kv_norm_factor(large ? squares[1] : squares[0], 1.f / D, large ? 0.f : p.norm.eps) * (large ? kKvTiny / kHeld : 1.f / kHeld);
+            const bool large = kv_norm_leaves(squares[0], 1.f / D, p.norm.eps);
+            factor = kv_norm_factor(large ? squares[1] : squares[0], 1.f / D, kv_norm_eps(large, p.norm.eps)) * (large ? kKvTiny / kHeld : 1.f / kHeld);
         }
         const int e = (int)(__float_as_uint(m) >> 23) - 127;                          // m in [2^e, 2^(e + 1))
         const int up = e < -100 ? 114 : e > 127 ? 0 : 14 - e;                         // (not finite: as it is, the row becomes NaN)
