@@ -490,7 +490,8 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
  *
  * Reserve: makes every page that the batch's new tokens fall in exist and be the sequence's own; call it before svdq_kv_append.  Among the entries of positions kv_len - n ..
  * kv_len - 1, those that name no page, or one whose count is above one, get the lowest pages that were free at the call, in the order of sequences and entries; the old page's
- * count goes down.  Of a page that held tokens before the new ones, those are copied, in whole blocks of 32, in `cache` if it is given; copies (NULL, or device int32 [sequences][3])
+ * count goes down.  Where every entry that names a shared page is among those, in the same column (as after a fork whose parent was released), the first of the sequences keeps it.  Of a
+ * page that held tokens before the new ones, those are copied, in whole blocks of 32, in `cache` if it is given; copies (NULL, or device int32 [sequences][3])
  * says for each sequence (page, to page, tokens), (-1, -1, 0) if nothing is to be copied: with svdq_kv_copy_pages the caches of further layers follow.  missing (NULL, or device int32)
  * becomes the number of entries for which no page was left: they name none (the tokens there are neither written nor seen, and those that a shared page held are lost to the
  * sequence), nobody else's pages are touched.  A sequence's first entry that names no page while tokens before the new ones fall in it gets none either, is counted in missing and stays as it

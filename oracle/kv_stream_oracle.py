@@ -145,16 +145,21 @@ class Pages:
 
     def reserve(self, table, new, lens):
         """The copies (page, to page, tokens) of every sequence, and how many entries got no page.  An entry that names no page, of a page whose first tokens are no new ones, gets
-        none: nothing holds those tokens, and a page that was another's would show its."""
+        none: nothing holds those tokens, and a page that was another's would show its.  Where all entries that name a shared page are such ones, of one place in their rows, the first
+        sequence keeps it."""
         free = [g for g, n in enumerate(self.refs) if n <= 0]
-        was, missing, copies = list(self.refs), 0, []
-        for row, n, length in zip(table, new, lens):
-            length = min(max(length, 0), len(row) * self.P)
+        was, missing, copies, holders = list(self.refs), 0, [], {}
+        lens = [min(max(n, 0), len(row) * self.P) for row, n in zip(table, lens)]
+        entries = [range(max(length - n, 0) // self.P, (length + self.P - 1) // self.P) if n > 0 else () for n, length in zip(new, lens)]
+        for b, row in enumerate(table):
+            for e in entries[b]:
+                holders.setdefault((e, row[e]), []).append(b)
+        for b, (row, n, length) in enumerate(zip(table, new, lens)):
             before = max(length - n, 0)
             copy = (-1, -1, 0)
-            for e in range(before // self.P, (length + self.P - 1) // self.P) if n > 0 else ():
+            for e in entries[b]:
                 g = row[e]
-                if self.page(g) and was[g] <= 1:
+                if self.page(g) and (was[g] <= 1 or len(holders[e, g]) == was[g] and b == holders[e, g][0]):
                     continue
                 if not self.page(g) and e * self.P < before:
                     missing += 1

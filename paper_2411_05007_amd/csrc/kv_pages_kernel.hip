@@ -4,14 +4,15 @@
 //   fork      a row of a table becomes the pages of another row's tokens; their counts go up
 //   release   entries of pages wholly within a range of tokens are cleared; their counts go down
 //   reserve   every entry that a batch's new tokens fall in names a page of the sequence's own: entries that name none, or one with a count above one, get the lowest free pages, in the
-//             order of sequences and entries, and what a shared page held before the new tokens is copied.  A sequence's first entry that names none while tokens before the new ones fall in
-//             it (they found no page, or it was given back) gets none: nothing could fill those tokens' places, and another sequence's would be seen there
+//             order of sequences and entries, and what a shared page held before the new tokens is copied.  Where all the entries that name a page are to leave it, the first sequence
+//             keeps it.  A sequence's first entry that names none while tokens before the new ones fall in it (they found no page, or it was given back) gets none: nothing could
+//             fill those tokens' places, and another sequence's would be seen there
 //   copy      pages of one cache into pages of the same or another one
 // Reserve is two kernels.  The first notes what is free (a bit a page, counts for each 1024) and which entries lack a page (a bit an entry, a count for each sequence), the second
 // sums what comes before its sequence, enumerates the free pages from there and the entries side by side through LDS, and writes table and counts; further workgroups of the
 // sequence find the one page that they copy to by themselves.  Decisions are made from the first one's notes alone, so the order in which workgroups change tables and counts does not matter.
-// Bound: latency, of two launches; then memory, for the copies.  32 branches of eight sequences: release 2.3, fork 2.6, notes 3.0, reserve 4.8 us with 5.8 MB read and written (16.4 where every step of
-// the search waited for the one before); 256 branches, pages of 256: 4.0, 3.4, 3.3 and 16 us with 80 MB read and written, 4.9 TB/s.
+// Bound: latency, of two launches; then memory, for the copies.  32 branches of eight sequences: release 2.3, fork 2.6, notes 3.5 (3.2 without the search for a shared page's last holders), reserve 4.7 us with 5.8 MB read and written (16.4 where every step of
+// the search waited for the one before); 256 branches, pages of 256: 4.0, 3.4, 4.4 (3.2; 5.7 with 64 sequences asked for at a time) and 16 us with 80 MB read and written, 4.9 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -56,16 +57,17 @@ __global__ __launch_bounds__(256) void kv_fork_kernel(KvForkParams p) {
 constexpr int kSlicePages = 1024;      // pages of a count
 constexpr int kLost = -2;              // in the place of a shared page: the first entry is to stay without one
 struct Entries { int lo, hi, before; };      // of a sequence's table that its new tokens fall in; tokens before them
-__device__ __forceinline__ Entries entries_of(const KvReserveParams &p, int b) {
-    const int cu0 = p.batch.cu[b], cu1 = p.batch.cu[b + 1], kv_len = p.batch.kv_len[b];
-    const int t0 = kv_within(cu0, 0, p.batch.total), n = __builtin_amdgcn_readfirstlane(kv_within(cu1, t0, p.batch.total) - t0);
+__device__ __forceinline__ Entries entries_between(const KvReserveParams &p, int cu0, int cu1, int len) {
+    const int t0 = kv_within(cu0, 0, p.batch.total), n = kv_within(cu1, t0, p.batch.total) - t0;
     const long long most = (long long)p.batch.table_width << p.pool.page_shift;
-    int len = __builtin_amdgcn_readfirstlane(kv_len);
     len = len < 0 ? 0 : (long long)len > most ? (int)most : len;
     const int before = len > n ? len - n : 0;
     Entries e = {before >> p.pool.page_shift, (int)(((long long)len + (1 << p.pool.page_shift) - 1) >> p.pool.page_shift), before};
     if (n == 0 || e.hi < e.lo) e.hi = e.lo;
     return e;
+}
+__device__ __forceinline__ Entries entries_of(const KvReserveParams &p, int b) {      // b the same in all lanes
+    return entries_between(p, __builtin_amdgcn_readfirstlane(p.batch.cu[b]), __builtin_amdgcn_readfirstlane(p.batch.cu[b + 1]), __builtin_amdgcn_readfirstlane(p.batch.kv_len[b]));
 }
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(kv_sum_upto(x), 63); }
 
@@ -93,7 +95,37 @@ __global__ __launch_bounds__(256) void kv_reserve_plan_kernel(KvReserveParams p)
     }
     const int b = ((int)blockIdx.x - p.slices) * 4 + wave;      // entries that lack a page
     if (b >= p.batch.sequences) return;
+    // A page that a sequence would leave is looked for in the same entry of the others (a branch has it where its parent does), 64 of them at a time: the first 64 are asked for in time.
+    const int last = p.batch.sequences - 1;
+    struct Peer { int cu0, cu1, len, page; };
+    const auto ask = [&](int j, int e) { return Peer{p.batch.cu[j], p.batch.cu[j + 1], p.batch.kv_len[j], p.batch.table[(size_t)j * p.batch.table_width + e]}; };
     const Entries at = entries_of(p, b);
+    const Peer first_peer = ask(lane < last ? lane : last, at.lo < at.hi ? at.lo : 0);
+    // The batch has all the entries that name the page, and b is the first sequence of them: it keeps the page.
+    const auto keeps = [&](int e, int page, int count) {
+        if (count > p.batch.sequences) return false;
+        int found = 0, first = -1;
+        const auto look = [&](const Peer &x, int j0) {
+            const Entries others = entries_between(p, x.cu0, x.cu1, x.len);
+            const unsigned long long word = __builtin_amdgcn_ballot_w64(j0 + lane <= last && e >= others.lo && e < others.hi && x.page == page);
+            if (first < 0 && word != 0ull) first = j0 + __builtin_ctzll(word);
+            found += __builtin_popcountll(word);
+        };
+        int j0 = 0;
+        if (e == at.lo) {
+            look(first_peer, 0);
+            j0 = 64;
+        }
+        constexpr int kAhead = 4;
+        for (; j0 <= last && (first < 0 || first == b); j0 += 64 * kAhead) {
+            Peer x[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) x[i] = ask(j0 + 64 * i + lane < last ? j0 + 64 * i + lane : last, e);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) look(x[i], j0 + 64 * i);
+        }
+        return first == b && found == count;
+    };
     const bool holds = (long long)at.lo << p.pool.page_shift < at.before;      // tokens before the new ones fall in the first entry
     int count = 0, shared = -1;
     for (int e0 = at.lo & ~63; e0 < at.hi; e0 += 64) {
@@ -101,7 +133,12 @@ __global__ __launch_bounds__(256) void kv_reserve_plan_kernel(KvReserveParams p)
         bool lacks = e >= at.lo && e < at.hi;
         const int page = lacks ? p.batch.table[(size_t)b * p.batch.table_width + e] : -1;
         const bool named = is_page(page, p.pool.pages);
-        if (named) lacks = p.pool.refs[page] > 1;
+        const int refs = named ? p.pool.refs[page] : 0;
+        if (named) lacks = refs > 1;
+        for (unsigned long long left = __builtin_amdgcn_ballot_w64(named && lacks); left != 0ull; left &= left - 1) {
+            const int i = __builtin_ctzll(left);
+            if (keeps(e0 + i, __builtin_amdgcn_readlane(page, i), __builtin_amdgcn_readlane(refs, i)) && lane == i) lacks = false;
+        }
         const bool lost = lacks && !named && holds && e == at.lo;
         lacks = lacks && !lost;
         if (__builtin_amdgcn_ballot_w64(lost) != 0ull) shared = kLost;

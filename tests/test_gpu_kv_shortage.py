@@ -116,11 +116,14 @@ class World:
         kc, ks, vc, vs = (t.cpu().numpy() for t in (self.cache.k_codes, self.cache.k_scales, self.cache.v_codes, self.cache.v_scales))
         shape = (len(keys), self.H)
         k, v, kb, vb = np.zeros(shape + (self.D,)), np.zeros(shape + (self.D,)), np.zeros(shape, np.int64), np.zeros(shape, np.int64)
+        blocks = {}
         for i, t in enumerate(keys):
             page, at = row[t // self.P], t % self.P // 32
             for h in range(self.H):
                 kb[i, h], vb[i, h] = ks[page, h, at], vs[page, h, at]
-                a, b = K.block_numbers(kc[page, h, at], vc[page, h, at])
+                if (page, h, at) not in blocks:
+                    blocks[page, h, at] = K.block_numbers(kc[page, h, at], vc[page, h, at])
+                a, b = blocks[page, h, at]
                 k[i, h], v[i, h] = a[t % 32] * 2.0 ** (kb[i, h] - 127), b[t % 32] * 2.0 ** (vb[i, h] - 127)
         return k, v, kb, vb
 
@@ -237,3 +240,77 @@ def test_a_reservation_that_is_tried_again(torch, KV):
     x = w.random(70)
     out = w.launch(x, batch)
     assert w.look(t, [70, 0], x, out) == 0 and t.have[0] == set(range(90))
+
+
+# ---- the last holders of a page ------------------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("free", [0, 1])
+def test_the_last_holders_of_a_page_leave_it_to_the_first_of_them(torch, KV, free):
+    """Two branches of a prompt that has ended write beside each other: one keeps the page, the other copies it, or, in a full pool, is the only one that loses its tokens there."""
+    P = 64
+    w = World(torch, KV, 2 + free, P, seed=7)
+    t, c = w.rows(2, 2), w.rows(2, 3)
+    w.step(t, [40, 0])
+    w.step(t, [0, 30], scale=8.0)
+    w.fork(t, [0, 0], c)
+    w.end((t, 0))
+    for new in ([1, 1], [3, 0], [0, 5], [7, 9]):
+        assert w.step(c, new) == (0 if free or new[1] == 0 else 1)
+    assert c.have[0] == set(range(51)) and c.have[1] == (set(range(55)) if free else set())
+    w.end((c, 0), (c, 1), (t, 1))
+    assert not w.pool.refs.any()
+
+
+def test_many_branches_that_outlive_their_prompt(torch, KV):
+    """130 of them, cut back into a page that they share and past others; the first ones stand still for a while."""
+    P, B = 32, 130
+    w = World(torch, KV, 900, P, H=1, G=1, seed=8)
+    t, c = w.rows(1, 8), w.rows(B, 8)
+    w.step(t, [200])
+    w.fork(t, [0] * B, c)
+    w.end((t, 0))
+    c.lens = [100 + b % 3 for b in range(B)]
+    c.have = [{k for k in held if k < n} for held, n in zip(c.have, c.lens)]
+    assert w.step(c, [0, 0] + [1 + b % 41 for b in range(2, B)]) == 0
+    assert w.step(c, [1] * B) == 0 and c[0, 3] != c[1, 3]
+    assert w.step(c, [5 * (b % 7) for b in range(B)]) == 0
+
+
+@pytest.mark.parametrize("B", [3, 64, 65])
+def test_the_page_of_a_prefix_in_a_captured_step(torch, KV, B):
+    """Branches go on alone, a token of each a replay, and all take over another's tokens between two of them: as many pages as they need if one of them keeps what is shared."""
+    P = 32
+    w = World(torch, KV, B + 1, P, H=1, G=1, seed=9 + B)
+    t, c = w.rows(1, 4), w.rows(B, 4)
+    w.step(t, [45])
+    w.fork(t, [0] * B, c)
+    length = i32(torch, c.lens)
+    batch = KV.KVBatch(i32(torch, range(B + 1)), length, c, B, 1, 4 * P)
+    x, out, one = w.random(B), torch.empty(B, 1, w.D, dtype=torch.bfloat16, device=DEV), i32(torch, [1] * B)
+    pages, ws = w.pool.reserve_workspace(batch), w.cache.attention_workspace(batch, 1)
+    idle = KV.KVBatch(i32(torch, [0] * (B + 1)), i32(torch, [0] * B), torch.full_like(c, -1), B, 1, 4 * P)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):      # (the first call of a kernel loads it)
+        w.launch(x, idle, out, pages, ws)
+        length.add_(one)
+        length.sub_(one)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        length.add_(one)
+        w.launch(x, batch, out, pages, ws)
+    w.end((t, 0))
+    for i in range(4):
+        if i == 2:      # everyone takes over the last one's tokens
+            t2 = w.rows(B, 4)
+            w.fork(c, [B - 1] * B, t2)
+            w.end(*((c, b) for b in range(B)))
+            w.fork(t2, list(range(B)), c)
+            w.end(*((t2, b) for b in range(B)))
+            length.copy_(i32(torch, c.lens))
+        x.copy_(w.random(B))
+        c.lens = [n + 1 for n in c.lens]
+        graph.replay()
+        assert w.look(c, [1] * B, x, out) == 0 and len(set(c[:, 1].tolist())) == B

@@ -27,3 +27,28 @@ def test_a_call_that_is_repeated():
     assert p.reserve(t, [40, 20], [40, 20])[1] == 1 and t == [[0, 1], [-1, -1]]
     p.release(t, [32, 0])
     assert p.reserve(t, [0, 20], [32, 20])[1] == 0 and t == [[0, -1], [1, -1]]
+
+
+def test_the_last_holders_of_a_page_leave_it_to_the_first_of_them():
+    p = W.Pages(3, 32)
+    t, c, lens = [[-1] * 2], [[-1] * 2 for _ in range(3)], [0] * 3
+    p.reserve(t, [20], [20])
+    p.fork(t, [20], [0, 0, 0], c, lens)
+    assert p.refs == [4, 0, 0]
+    p.release(t)
+    assert p.reserve(c, [0, 1, 1], [20, 21, 21]) == ([(-1, -1, 0), (0, 1, 20), (0, 2, 20)], 0) and p.refs == [1, 1, 1]      # (the first one stands still)
+    p.release(c, [0, 0, 64])
+    d, lens = [[-1] * 2 for _ in range(3)], [0] * 3
+    p.fork(c, [0, 0, 21], [2, 2, 2], d, lens)
+    p.release(c)
+    assert p.refs == [0, 0, 3]
+    assert p.reserve(d, [1, 1, 20], [22, 22, 41]) == ([(-1, -1, 0), (2, 0, 21), (2, 1, 21)], 1) and d == [[2, -1], [0, -1], [1, -1]] and p.refs == [1, 1, 1]
+
+
+def test_a_holder_that_is_not_there_keeps_the_page_shared():
+    p = W.Pages(4, 32)
+    p.refs = [3, 0, 0, 0]
+    assert p.reserve([[0, -1], [0, -1]], [1, 1], [5, 9]) == ([(0, 1, 4), (0, 2, 8)], 0) and p.refs == [1, 1, 1, 0]
+    p.refs = [2, 0, 0, 0]
+    t = [[-1, 0], [0, -1]]      # at other places: as of any page with a count above one
+    assert p.reserve(t, [1, 1], [33, 1]) == ([(-1, -1, 0)] * 2, 0) and t == [[-1, 1], [2, -1]] and p.refs == [0, 1, 1, 0]
