@@ -502,7 +502,7 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
  * and counts of a captured graph's buffers it can be captured with the step.
  *
  * Copy: tokens c[i][2] (in whole blocks) of page c[i][0] of `from` to page c[i][1] of `to`; nothing where either names no page.  The caches are the same one or alike; no page is
- * written twice, or written and read.
+ * written twice, or written and read, and what is written no other row shares.
  */
 typedef struct {
     int32_t *refs; /* device [pages] */
@@ -524,6 +524,9 @@ int svdq_kv_copy_pages(const svdq_kv_cache_dev *to, const svdq_kv_cache_dev *fro
  * With a rope, keys are turned from the position that the token had to the one that it gets (the table that they were appended with; its rows need not have size one); a token
  * that keeps its position keeps its key.  Blocks are quantized as by an append of the moved vectors in that order: tokens before to_first[b] in its block stay, at the larger
  * byte; what lies behind the last move in its block is lost.  A token that no page of from_table holds becomes one with NaN codes, as do those that have some.
+ * Every page that is written is named by one table entry only, the sequence's: what other rows share (a count above one) would change under them.  A branch is thinned out beside others
+ * into a row of its own: fork the tokens that stay in front of the moves (or begin with an empty row), reserve as many new tokens as there are moves, compact from the old row to the new one,
+ * release the old one.
  *   workspace NULL: no page that is written is one that is read.  Otherwise (device, 256-byte aligned, >= svdq_kv_compact_workspace_bytes(), no initial contents; calls that share
  *   one are ordered on one stream) pages may be read and written in the same call, as where a sequence shrinks in place; no page is written for two sequences.
  * One kernel, a second one with a workspace.  SVDQ_EINVAL and SVDQ_EUNSUPPORTED as above, SVDQ_EINVAL also for caches that do not fit each other.

@@ -210,7 +210,8 @@ class KVCache:
         return out
 
     def copy_pages(self, copies, source: Optional["KVCache"] = None, stream=None) -> None:
-        """copies int32 [n, 3] on the GPU: page of `source` (None: of this cache), page of this cache, tokens (whole blocks of 32 are copied; rows that name no page are skipped)."""
+        """copies int32 [n, 3] on the GPU: page of `source` (None: of this cache), page of this cache, tokens (whole blocks of 32 are copied; rows that name no page are skipped).
+        No other row of a table names a page that is written."""
         _device_int32(copies, "copies")
         assert copies.dim() == 2 and copies.shape[1] == 3, "copies: [n, 3]"
         S._check(S.lib().svdq_kv_copy_pages(self.cdesc, (source or self).cdesc, copies.data_ptr(), copies.shape[0], self._stream(stream)), "svdq_kv_copy_pages")
@@ -223,7 +224,8 @@ class KVCache:
 
     def compact(self, moves: KVMoves, rope: Optional[Rope] = None, source: Optional["KVCache"] = None, workspace=None, stream=None) -> None:
         """Moves tokens into pages of this cache, out of pages of `source` (None: of this cache).  rope: turns their keys to the new positions.  workspace (compact_workspace()):
-        needed where pages that are written are read as well."""
+        needed where pages that are written are read as well.  Pages that are written are named by no other row: a branch whose pages others share is compacted into a row of its own,
+        which reserve() fills, and its old row is released."""
         assert moves.lists in (1, self.kv_heads), f"from_token: {moves.lists} lists for {self.kv_heads} heads"
         assert workspace is None or (workspace.dtype is torch.uint8 and workspace.is_cuda and workspace.is_contiguous()), "workspace: uint8 on the GPU"
         at, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
