@@ -324,8 +324,8 @@ int copy_parts(long long copies, const KvCache &c) {
 KvReservePlan plan_kv_reserve(int pages, int sequences, int width) {
     KvReservePlan r{};
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-    r.slices = (pages + kSlicePages - 1) / kSlicePages;
-    r.words = (width + 63) / 64;
+    r.slices = (int)(((long long)pages + kSlicePages - 1) / kSlicePages);
+    r.words = (int)(((long long)width + 63) / 64);
     r.slice_off = up((size_t)r.slices * (kSlicePages / 64) * 8);
     r.count_off = r.slice_off + up((size_t)r.slices * 4);
     r.shared_off = r.count_off + up((size_t)sequences * 4);
