@@ -12,9 +12,10 @@
 // Moves within the same pages go by way of the workspace: every block is made there first, a second kernel puts them in place, and their order does not matter.
 // Of values every line of an old block holds all of its tokens, so blocks are read whole, and twice where neighbouring new blocks share one.  The rows of the next head are in flight
 // while this one's are picked and written.
-// Bound: memory.  64 sequences of 9000 to 16384 tokens, eight heads of 128, of which 5000 to 12001 stay, keys turned: 622 us; 2.2 GB pass the L2s in that time, 3.6 TB/s, where the plain
-// reading back of the same rows reaches 4.05 (without turning 580 us, 4.0 TB/s where the latest stay).  At 128 registers four workgroups stay on a CU (three, at 131: 780 us; five spill).
-// 16 sequences with lists for each head, two fifths kept: 76 us, 2.3 TB/s, a chain of tokens, pages, blocks and their picking for each head, eleven rounds of workgroups (two to four heads a
+// Bound: memory.  64 sequences of 9000 to 16384 tokens, eight heads of 128, of which 5000 to 12001 stay, keys turned: 622 us, in which 3.4 GB pass the L2s (2.32 read,
+// 1.11 written), 5.5 TB/s; the plain reading back of the same rows moves 3.35 GB at 5.0.  It is more than it needs: the keys that stay and old blocks of values, whole and once, are 1.36 GB; the rotation's
+// rows, two a token, are 0.48, and the rest are old blocks that two new ones share (without turning 595 us, 2.95 GB; where the latest stay, 567 and 2.7).  At 128 registers four workgroups stay on a CU (three, at 131: 780 us; five spill).
+// 16 sequences with lists for each head, two fifths kept: 76 us, 267 MB (183 read), 3.5 TB/s, a chain of tokens, pages, blocks and their picking for each head, eleven rounds of workgroups (two to four heads a
 // workgroup 75 to 79).  A few tokens of 32 sequences: 7.8 us, and 4.0 to put them in place.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -11,8 +11,9 @@
 // Reserve is two kernels.  The first notes what is free (a bit a page, counts for each 1024) and which entries lack a page (a bit an entry, a count for each sequence), the second
 // sums what comes before its sequence, enumerates the free pages from there and the entries side by side through LDS, and writes table and counts; further workgroups of the
 // sequence find the one page that they copy to by themselves.  Decisions are made from the first one's notes alone, so the order in which workgroups change tables and counts does not matter.
-// Bound: latency, of two launches; then memory, for the copies.  32 branches of eight sequences: release 2.3, fork 2.6, notes 3.5 (3.2 without the search for a shared page's last holders), reserve 4.7 us with 5.8 MB read and written (16.4 where every step of
-// the search waited for the one before); 256 branches, pages of 256: 4.0, 3.4, 4.4 (3.2; 5.7 with 64 sequences asked for at a time) and 16 us with 80 MB read and written, 4.9 TB/s.
+// Bound: latency, of two launches; then memory, for the copies.  32 branches of eight sequences: release 2.3, fork 2.6, notes 3.5 (3.2 without the search for a shared page's last holders), reserve
+// 4.7 us with 5.9 MB read and written (16.4 where every step of the search waited for the one before); 256 branches, pages of 256: 4.0, 3.4, 4.4 (3.2; 5.7 with 64 sequences asked for at a time) and
+// 16 us, in which 80 MB pass the L2s, 5.0 TB/s.  40 of those are reads, though the pages that four branches share are 10: the four are on different XCDs, and each L2 fetches its own.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -16,7 +16,8 @@
 // arrived joins them in chunk order (the same bits whoever it is), eight requests in flight a thread; nothing waits for another workgroup.
 // First tokens that stay visible before a window are blocks before the window's: the chunks count on over the gap, which is not read.
 // Bound: memory, one byte per channel of a key and a value: one sequence of 131071 keys, 8 key heads of 128, 32 query heads 54 us (5.0 TB/s), 64 sequences
-// of 100 to 16384 keys 245 us (4.65 TB/s); of 100 to 32768 in a window of 8192 with 64 first tokens and normalised queries 195 us (4.83 TB/s, 193 without either).  Short ones by a chain of round trips: 5.7 us for one block (lengths, table, codes, queries turned on the way), 9.3 us for 777 keys of eight
+// of 100 to 16384 keys 245 us (4.65 TB/s); of 100 to 32768 in a window of 8192 with 64 first tokens and normalised queries 195 us (4.83 TB/s, 193 without either).  A norm alone, without a window,
+// adds 0.3 % there (231.3 us and 232.0, the last-level cache holding a part) and 0.6 us to a short call (777 keys 9.6 and 10.2).  Short ones by a chain of round trips: 5.7 us for one block (lengths, table, codes, queries turned on the way), 9.3 us for 777 keys of eight
 // heads, where the eight CUs draw 52 GB/s each; 11.4 for 1024 keys and four first tokens, normalised queries, in five pieces (10.9 without).  Eight wavefronts a workgroup gain nothing: 13.0.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -48,7 +49,7 @@ constexpr int rows_lds_bytes(int D, int waves, int cap, int chunks, bool norm) {
 constexpr int kAgent = 16;      // cache policy of a buffer access that all XCDs see
 
 // As KvRotating, of a row that is normalised first.  The factor r of the norm is the same for all channels of a row, so it waits: what is turned is x w 2^-32 (which no finite x takes past
-// fp32), and r 2^32 goes into the row's factor of the scores, when the wavefronts' sums of squares have met beside their maxima.
+// fp32 with weights up to 2^32), and r 2^32 goes into the row's factor of the scores, when the wavefronts' sums of squares have met beside their maxima.
 // Every load is made whatever the call needs (from `any`, 32 D bytes that may be read, where there is nothing else), so that no branch lies between the block table's entry, which
 // is waited for next, and what was asked for behind it.
 constexpr float kHeld = 2.3283064365386963e-10f;      // 2^-32

@@ -13,7 +13,7 @@
 // Few row tiles on many keys take parts of the keys, which kv_meet_kernel joins.  A wavefront whose rows are past the sequence's only carries codes.
 // Bound: matrix cores and vector ALU, which overlap little, at the chip's power limit (1.9 of 2.4 GHz under the profiler).  8192 tokens, 32 query heads on 8, on 16384 keys 1540 us, 1.07 PFLOP/s
 // (a library product of 8192 cubed in f16 reaches 1.215): matrix cores busy 51 % of the time, vector ALU 55 %; 4608 tokens of 24 heads, all with all, 280 us, 48 and 54 %, and 432
-// tiles are two rounds of 256 CUs; the same 8192 tokens in a window of 8192 on 24576, 128 first tokens and normalised queries, 1072 us, 1.04 PFLOP/s (masked scores take one compare and one
+// tiles are two rounds of 256 CUs; normalised queries, with first tokens of their own weights, add 2 us; the same 8192 tokens in a window of 8192 on 24576, 128 first tokens and normalised queries, 1058 to 1087 us, 1.03 to 1.06 PFLOP/s (masked scores take one compare and one
 // select each: with a branch for each, as the compiler made of "in the window or a first token", 1195); six ragged chunks of up to 2111 tokens 350 us, 43 and 58 %; heads of 64, 8192 tokens on 16384 keys 1036 us, 34 and 68 %.  What a workgroup of 128 rows costs beside its tiles (1.05 us each): scan over
 // the sequences 1.2 us, queries and first pages 2.2, turning 2.5, first codes 1.4, out 2, of which the other workgroup of the CU covers about two thirds.
 #include <hip/hip_runtime.h>
