@@ -492,7 +492,8 @@ int svdq_kv_attention_normed(const svdq_kv_cache_dev *cache, const svdq_kv_batch
  * kv_len - 1, those that name no page, or one whose count is above one, get the lowest pages that were free at the call, in the order of sequences and entries; the old page's
  * count goes down.  Where every entry that names a shared page is among those, in the same column (as after a fork whose parent was released), the first of the sequences keeps it.  Of a
  * page that held tokens before the new ones, those are copied, in whole blocks of 32, in `cache` if it is given; copies (NULL, or device int32 [sequences][3])
- * says for each sequence (page, to page, tokens), (-1, -1, 0) if nothing is to be copied: with svdq_kv_copy_pages the caches of further layers follow.  missing (NULL, or device int32)
+ * says for each sequence (page, to page, tokens), (-1, -1, 0) if nothing is to be copied: with svdq_kv_copy_pages the caches of further layers follow,
+ * each before anything is appended to it (a page that is copied may be another sequence's to write); where no copy is made, those tokens' places hold what the new page held.  missing (NULL, or device int32)
  * becomes the number of entries for which no page was left: they name none (the tokens there are neither written nor seen, and those that a shared page held are lost to the
  * sequence), nobody else's pages are touched.  A sequence's first entry that names no page while tokens before the new ones fall in it gets none either, is counted in missing and stays as it
  * is: those tokens are nowhere, and a page that was another sequence's would show its tokens in their place.  So after a shortage a sequence goes on without the rest of that page, in every

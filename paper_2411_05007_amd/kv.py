@@ -309,7 +309,7 @@ class KVPages:
 
     def reserve(self, cache, batch: KVBatch, missing=None, workspace=None, stream=None) -> None:
         """Pages of its own for every new token of the batch, whose block_table is written; tokens before them in a shared page are copied, in `cache` or, where layers
-        have caches of their own, in each of a list of them.  missing: int32 [1] on the GPU, entries for which no page was left (they name none), and those that cannot have
+        have caches of their own, in each of a list of them (in none of an empty list).  missing: int32 [1] on the GPU, entries for which no page was left (they name none), and those that cannot have
         one: a sequence's first that names none while tokens before the new ones fall in it.  Written anew by each call: a captured step adds it up in a tensor of its own."""
         caches = [cache] if isinstance(cache, KVCache) else list(cache)
         for c in caches:
